@@ -68,7 +68,9 @@ typedef enum coded_status {
 typedef enum coded_dtype {
     CODED_F32 = 0,
     CODED_BF16 = 1,            /* bfloat16 bit patterns (uint16) */
-    CODED_F64 = 2
+    CODED_F64 = 2,
+    CODED_MX4 = 3,             /* microscaled 4-bit codes (the coded_mx_* calls alone) */
+    CODED_MX8 = 4              /* microscaled 8-bit codes (the coded_mx_* calls alone) */
 } coded_dtype;
 
 /* Largest n supported (survivor and worker lists travel as kernel arguments). */
@@ -479,6 +481,92 @@ coded_status coded_shuffle_encode(const float* A, int64_t q, int64_t r, int64_t 
 coded_status coded_shuffle_decode(const float* A, int64_t q, int64_t r, int64_t lda, const float* M, int64_t ldm,
                                   const int64_t* enc_off, const int32_t* enc_rows, const int32_t* term_msg,
                                   int64_t coded_rows, int64_t terms, float* out, int64_t ldo, void* stream);
+
+/* ---------------------------------------------------------------- microscaled matrices
+ * A matrix of q x r in blocks of 32 consecutive columns of a row that share a
+ * scale (the block format of the OCP Microscaling Formats specification 1.0),
+ * so that the products, which are bound by reading A, read an eighth (MX4) or
+ * a quarter (MX8) of its fp32 bytes, and a batch that is kept for the backward
+ * pass takes half (MX8) of its bf16 bytes.
+ *   codes   row t at byte t*ldc (ldc a multiple of 16, codes 16-byte aligned).
+ *           CODED_MX4: E2M1, column c in byte c/2, an even column in its low
+ *           bits; values 0 .5 1 1.5 2 3 4 6 and their negatives.  CODED_MX8:
+ *           E4M3, column c in byte c; values up to 448.  The codes that fill
+ *           the last block of a row past column r are zero.
+ *   scales  row t at byte t*lds (lds a multiple of 4, scales 4-byte aligned);
+ *           byte b is the scale 2^(b - 127) of columns 32b .. 32b + 31, 255 a
+ *           block without values: each of them counts as NaN.
+ * coded_mx_sizes gives the smallest pitches.  A row of a matrix, or any run of
+ * rows, is such a matrix at its own first row, so a block row of A is used as
+ * it lies.  Products take A's values as they are: a code times its scale is a
+ * bfloat16 value (scales below 2^-117, which coded_mx_quantize does not write,
+ * may give values that are too small to be one).
+ * Right-hand sides and results: columns of X (k x s, row stride ldx >= s) and of
+ * Y (n x s, ldy >= s) unless `order` says that a right-hand side is a row of X
+ * (CODED_X_ROWS: s x k, ldx >= k) or of Y (CODED_Y_ROWS: s x n, ldy >= n), as
+ * where tokens are rows.  Sizes up to 2^40 each; any of them may be 0, and a
+ * sum of no terms is 0.
+ */
+#define CODED_X_ROWS 1
+#define CODED_Y_ROWS 2
+
+/* Bytes from row to row of the codes and scales of a matrix of r columns, at
+ * the least.  Either output may be NULL. */
+coded_status coded_mx_sizes(coded_dtype fmt, int64_t r, int64_t* code_pitch, int64_t* scale_pitch);
+
+/*
+ * coded_mx_quantize -- codes and scales of A (device, q x r of dt = CODED_F32
+ * or CODED_BF16, row stride lda).  With m the largest magnitude of a block the
+ * scale is 2^e, e = floor(log2 m) - 2 (MX4) or - 8 (MX8), at least -117; the
+ * codes are v / 2^e to nearest, ties to even, cut down to the largest value.  A
+ * block with an infinity or NaN in it gets the scale 255.  Writes the codes
+ * and scales of whole blocks (and scale bytes of 0 up to the next multiple of
+ * four), nothing else of a row.
+ */
+coded_status coded_mx_quantize(coded_dtype dt, const void* A, int64_t q, int64_t r, int64_t lda, coded_dtype fmt,
+                               void* codes, int64_t ldc, uint8_t* scales, int64_t lds, void* stream);
+
+/* The values, as dt = CODED_BF16 (exact, see above) or CODED_F32 (exact), into
+ * out (q x r, row stride ldo). */
+coded_status coded_mx_dequantize(coded_dtype fmt, const void* codes, int64_t ldc, const uint8_t* scales, int64_t lds,
+                                 int64_t q, int64_t r, coded_dtype dt, void* out, int64_t ldo, void* stream);
+
+/* Bytes of device workspace that coded_mx_mm (transposed == 0) or coded_mx_mm_t
+ * needs for these sizes (0: none, NULL will do). */
+coded_status coded_mx_workspace(int32_t transposed, coded_dtype fmt, int64_t q, int64_t r, coded_dtype x_dt, int64_t s,
+                                int32_t order, int64_t* bytes);
+
+/*
+ * coded_mx_mm -- Y = alpha * A X + beta * C, A (q x r) microscaled: a worker's
+ * product with its stored block (Sec. III-A), a layer's forward pass.
+ *   x_dt      CODED_F32 or CODED_BF16, or (with CODED_X_ROWS) CODED_MX4 or
+ *             CODED_MX8: X is then s x r in codes with pitch ldx and x_scales,
+ *             ldxs are its scales (else NULL, 0), as a batch that was saved.
+ *   y_dt      CODED_F32 or CODED_BF16.  Products are exact, sums are in fp32
+ *             (an fp32 X enters with all its bits), and a result is rounded
+ *             once, after alpha and beta.
+ *   C         of y_dt, in Y's order with row stride ldcc (0: one row that every
+ *             row of Y gets, a bias); may be Y itself.  Not read, and may be
+ *             NULL, when beta == 0.
+ *   workspace device, 16-byte aligned, coded_mx_workspace bytes.
+ * A NaN or infinity reaches the results whose sums it is part of and no other.
+ */
+coded_status coded_mx_mm(coded_dtype fmt, const void* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t q,
+                         int64_t r, coded_dtype x_dt, const void* X, int64_t ldx, const uint8_t* x_scales, int64_t ldxs,
+                         int64_t s, int32_t order, double alpha, double beta, const void* C, int64_t ldcc, void* Y,
+                         coded_dtype y_dt, int64_t ldy, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * coded_mx_mm_t -- Z = alpha * A^T U + beta * C from the same copy of A (q x r;
+ * U has q terms a right-hand side, Z has r results): the second product of a
+ * gradient step (Sec. III-E: A^T z), the gradient of a layer's input (A its
+ * weights, U the gradient of its output) and of its weights (A the saved batch).
+ * Arguments as coded_mx_mm's; u_dt is CODED_F32 or CODED_BF16.
+ */
+coded_status coded_mx_mm_t(coded_dtype fmt, const void* codes, int64_t ldc, const uint8_t* scales, int64_t lds,
+                           int64_t q, int64_t r, coded_dtype u_dt, const void* U, int64_t ldu, int64_t s, int32_t order,
+                           double alpha, double beta, const void* C, int64_t ldcc, void* Z, coded_dtype z_dt,
+                           int64_t ldz, void* workspace, int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

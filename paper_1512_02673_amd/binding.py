@@ -17,7 +17,8 @@ from .build import LIB_PATH
 
 CODED_OK, CODED_ERR_ARG, CODED_ERR_SHAPE, CODED_ERR_TOO_FEW, CODED_ERR_SINGULAR, CODED_ERR_HIP, \
     CODED_ERR_UNSUPPORTED = range(7)
-CODED_F32, CODED_BF16, CODED_F64 = 0, 1, 2
+CODED_F32, CODED_BF16, CODED_F64, CODED_MX4, CODED_MX8 = 0, 1, 2, 3, 4
+CODED_X_ROWS, CODED_Y_ROWS = 1, 2
 CODED_MAX_N = 128
 CODED_NOALLOC_SCRATCH_BYTES = 64 << 20
 CODED_PLANES_LO_BF16 = 3   # fp32 codes: hi plane fp32, lo plane bfloat16
@@ -65,6 +66,14 @@ _SIGNATURES = {
     "coded_simulate_runtimes": (_c_i32, [_c_i32, _c_i32, _c_u64, _c_u64, _c_i64, _c_dbl, _c_dbl, _c_p, _c_p, _c_p,
                                          _c_p]),
     "coded_optimal_k": (_c_i32, [_c_i32, _c_dbl, _c_p, _c_p, _c_p]),
+    "coded_mx_sizes": (_c_i32, [_c_i32, _c_i64, _c_p, _c_p]),
+    "coded_mx_quantize": (_c_i32, [_c_i32, _c_p, _c_i64, _c_i64, _c_i64, _c_i32, _c_p, _c_i64, _c_p, _c_i64, _c_p]),
+    "coded_mx_dequantize": (_c_i32, [_c_i32, _c_p, _c_i64, _c_p, _c_i64, _c_i64, _c_i64, _c_i32, _c_p, _c_i64, _c_p]),
+    "coded_mx_workspace": (_c_i32, [_c_i32, _c_i32, _c_i64, _c_i64, _c_i32, _c_i64, _c_i32, _c_p]),
+    "coded_mx_mm": (_c_i32, [_c_i32, _c_p, _c_i64, _c_p, _c_i64, _c_i64, _c_i64, _c_i32, _c_p, _c_i64, _c_p, _c_i64,
+                             _c_i64, _c_i32, _c_dbl, _c_dbl, _c_p, _c_i64, _c_p, _c_i32, _c_i64, _c_p, _c_i64, _c_p]),
+    "coded_mx_mm_t": (_c_i32, [_c_i32, _c_p, _c_i64, _c_p, _c_i64, _c_i64, _c_i64, _c_i32, _c_p, _c_i64, _c_i64,
+                               _c_i32, _c_dbl, _c_dbl, _c_p, _c_i64, _c_p, _c_i32, _c_i64, _c_p, _c_i64, _c_p]),
     "coded_status_string": (ctypes.c_char_p, [_c_i32]),
     "coded_last_error": (ctypes.c_char_p, []),
     "coded_version": (ctypes.c_char_p, []),
@@ -516,3 +525,167 @@ def coded_shuffle_decode(A, M, enc_off, enc_rows, term_msg, out, stream=None) ->
     _check(lib().coded_shuffle_decode(_ptr(A), q, r, lda, _ptr(M), ldm, _ptr(enc_off), _ptr(enc_rows), _ptr(term_msg),
                                       coded_rows, enc_rows.numel(), _ptr(out), ldo, _stream(stream)))
 
+
+
+# ---------------------------------------------------------------- microscaled matrices
+
+class MXMatrix:
+    """A microscaled matrix of `cols` columns: codes (uint8, rows x code pitch) and scales (uint8,
+    rows x scale pitch) in the layout of include/coded.h.  rows(a, b) is a run of its rows."""
+
+    __slots__ = ("codes", "scales", "cols", "fmt", "ldc", "lds")
+
+    def __init__(self, codes, scales, cols: int, fmt: int):
+        if fmt != CODED_MX4 and fmt != CODED_MX8:
+            raise ValueError("the format must be CODED_MX4 or CODED_MX8")
+        need_c, need_s = -(-cols // 32) * (16 if fmt == CODED_MX4 else 32), -(-cols // 128) * 4
+        uint8, n = _torch().uint8, codes.shape[0]
+        if codes.dtype != uint8 or codes.dim() != 2 or codes.shape[1] < need_c or (need_c and codes.stride(1) != 1):
+            raise ValueError(f"codes must be uint8, rows of at least {need_c} bytes")
+        if scales.dtype != uint8 or scales.dim() != 2 or scales.shape[1] < need_s or (need_s and scales.stride(1) != 1):
+            raise ValueError(f"scales must be uint8, rows of at least {need_s} bytes")
+        if scales.shape[0] != n:
+            raise ValueError("codes and scales must have the same number of rows")
+        self.codes, self.scales, self.cols, self.fmt = codes, scales, cols, fmt
+        self.ldc, self.lds = (codes.stride(0), scales.stride(0)) if n > 1 and cols > 0 else (need_c, need_s)
+
+    @property
+    def shape(self):
+        return self.codes.shape[0], self.cols
+
+    def rows(self, begin: int, end: int) -> "MXMatrix":
+        return MXMatrix(self.codes[begin:end], self.scales[begin:end], self.cols, self.fmt)
+
+    def _args(self):
+        return self.fmt, self.codes.data_ptr(), self.ldc, self.scales.data_ptr(), self.lds
+
+
+def _mx_dense(t, name):
+    """(rows, cols, row stride, type) of a 1-D (column) or row-major 2-D tensor; the stride of a
+    dimension of size 1 is not looked at."""
+    try:
+        dt = _dtype_code(t)
+    except KeyError:
+        raise ValueError(f"{name} must be float32 or bfloat16") from None
+    if t.dim() == 1:
+        rows, cols, ld, step = t.shape[0], 1, t.stride(0), 1
+    elif t.dim() == 2:
+        rows, cols = t.shape
+        ld, step = t.stride()
+    else:
+        raise ValueError(f"{name} must be 1-D or 2-D")
+    if cols > 1 and step != 1:
+        raise ValueError(f"{name} must be row-major")
+    return rows, cols, ld if rows > 1 else max(cols, 1), dt
+
+
+def coded_mx_sizes(fmt: int, r: int):
+    """(code pitch, scale pitch) in bytes of rows of r columns."""
+    c, s = ctypes.c_int64(), ctypes.c_int64()
+    _check(lib().coded_mx_sizes(fmt, r, ctypes.addressof(c), ctypes.addressof(s)))
+    return c.value, s.value
+
+
+def alloc_mx(q: int, r: int, fmt: int, device="cuda") -> MXMatrix:
+    """Room for a q x r microscaled matrix (not cleared: coded_mx_quantize writes all that is read)."""
+    torch = _torch()
+    c, s = coded_mx_sizes(fmt, r)
+    return MXMatrix(torch.empty((q, c), dtype=torch.uint8, device=device),
+                    torch.empty((q, s), dtype=torch.uint8, device=device), r, fmt)
+
+
+def coded_mx_quantize(A, M: MXMatrix, stream=None) -> None:
+    """Codes and scales of A (float32 or bfloat16) into M."""
+    q, r, lda, dt = _mx_dense(A, "A")
+    if M.shape != (q, r):
+        raise ValueError("M must have A's shape")
+    _check(lib().coded_mx_quantize(dt, A.data_ptr(), q, r, lda, *M._args(), _stream(stream)))
+
+
+def coded_mx_dequantize(M: MXMatrix, out, stream=None) -> None:
+    """M's values into out (float32 or bfloat16)."""
+    q, r, ldo, dt = _mx_dense(out, "out")
+    if M.shape != (q, r):
+        raise ValueError("out must have M's shape")
+    _check(lib().coded_mx_dequantize(*M._args(), q, r, dt, out.data_ptr(), ldo, _stream(stream)))
+
+
+def coded_mx_workspace(transposed: bool, fmt: int, q: int, r: int, x_dt: int, s: int, x_rows: bool = False,
+                       y_rows: bool = False) -> int:
+    """Bytes of workspace of coded_mx_mm, or of coded_mx_mm_t when transposed."""
+    b = ctypes.c_int64()
+    _check(lib().coded_mx_workspace(int(bool(transposed)), fmt, q, r, x_dt, s, bool(x_rows) | bool(y_rows) << 1,
+                                    ctypes.addressof(b)))
+    return b.value
+
+
+def _mx_side(t, name, by_rows):
+    """(terms, right-hand sides, row stride, type) of X or Y; a 1-D tensor is one right-hand side."""
+    rows, cols, ld, dt = _mx_dense(t, name)
+    if not by_rows:
+        return rows, cols, ld, dt
+    if t.dim() == 1:
+        if rows > 1 and ld != 1:
+            raise ValueError(f"{name} must be contiguous")
+        return rows, 1, max(rows, 1), dt
+    return cols, rows, ld, dt
+
+
+def _mx_product(transposed, M, X, Y, x_rows, y_rows, alpha, beta, C, workspace, stream):
+    q, r = M.shape
+    k, n = (q, r) if transposed else (r, q)
+    if isinstance(X, MXMatrix):
+        if not x_rows:
+            raise ValueError("a microscaled X holds a right-hand side a row: x_rows=True")
+        x_dt, xp, ldx, xsp, ldxs = X._args()
+        s, kx = X.shape
+    else:
+        kx, s, ldx, x_dt = _mx_side(X, "X", x_rows)
+        xp, xsp, ldxs = X.data_ptr(), None, 0
+    if kx != k:
+        raise ValueError(f"X must have {k} terms a right-hand side")
+    ny, sy, ldy, y_dt = _mx_side(Y, "Y", y_rows)
+    if ny != n or sy != s:
+        raise ValueError(f"Y must have {n} results for each of {s} right-hand sides")
+    cp, ldcc = None, 0
+    if beta != 0:
+        if C is None or C.dtype != Y.dtype:
+            raise ValueError("C must be given, of Y's type, when beta is not 0")
+        if C.shape == Y.shape:
+            ldcc = _mx_side(C, "C", y_rows)[2]
+        elif C.dim() == 1 and Y.dim() == 2 and C.shape[0] == Y.shape[1] and (C.shape[0] < 2 or C.stride(0) == 1):
+            ldcc = 0   # one row for every row of Y
+        else:
+            raise ValueError("C must have Y's shape, or be one row of it")
+        cp = C.data_ptr()
+    wsp, wsb = None, 0
+    if isinstance(workspace, str):
+        wsb = coded_mx_workspace(transposed, M.fmt, q, r, x_dt, s, x_rows, y_rows)
+        if wsb:
+            workspace = _torch().empty(wsb, dtype=_torch().uint8, device=Y.device)
+            wsp = workspace.data_ptr()
+    elif workspace is not None:
+        wsp, wsb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    order = bool(x_rows) | bool(y_rows) << 1
+    if transposed:
+        _check(lib().coded_mx_mm_t(*M._args(), q, r, x_dt, xp, ldx, s, order, alpha, beta, cp, ldcc, Y.data_ptr(), y_dt,
+                                   ldy, wsp, wsb, _stream(stream)))
+    else:
+        _check(lib().coded_mx_mm(*M._args(), q, r, x_dt, xp, ldx, xsp, ldxs, s, order, alpha, beta, cp, ldcc,
+                                 Y.data_ptr(), y_dt, ldy, wsp, wsb, _stream(stream)))
+
+
+def coded_mx_mm(M: MXMatrix, X, Y, x_rows: bool = False, y_rows: bool = False, alpha: float = 1.0, beta: float = 0.0,
+                C=None, workspace="auto", stream=None) -> None:
+    """Y = alpha * M X + beta * C.  X: r x s (or s x r with x_rows; then an MXMatrix too); Y: q x s (or s x q with
+    y_rows); C: like Y, or one row of it for every row.  A 1-D X, Y is one right-hand side.
+    workspace: "auto", or a device buffer of coded_mx_workspace bytes."""
+    _mx_product(False, M, X, Y, x_rows, y_rows, alpha, beta, C, workspace, stream)
+
+
+def coded_mx_mm_t(M: MXMatrix, U, Z, x_rows: bool = False, y_rows: bool = False, alpha: float = 1.0, beta: float = 0.0,
+                  C=None, workspace="auto", stream=None) -> None:
+    """Z = alpha * M^T U + beta * C.  U: q x s (or s x q with x_rows); Z: r x s (or s x r with y_rows)."""
+    if isinstance(U, MXMatrix):
+        raise ValueError("U must be float32 or bfloat16")
+    _mx_product(True, M, U, Z, x_rows, y_rows, alpha, beta, C, workspace, stream)

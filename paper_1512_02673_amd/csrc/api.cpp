@@ -75,6 +75,7 @@ size_t dtype_size(coded_dtype d) {
         case CODED_F32: return 4;
         case CODED_BF16: return 2;
         case CODED_F64: return 8;
+        default: return 0;
     }
     return 0;
 }
