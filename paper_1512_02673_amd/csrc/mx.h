@@ -49,6 +49,11 @@ hipError_t launch_mx_product(const MxArgs& a, hipStream_t st);
 // Workspace bytes the product may use (0: none).
 int64_t mx_workspace_bytes(const MxArgs& a);
 
+// Few right-hand sides (mx_few.hip): whether it serves these sizes, and its parts of the two above.
+bool mx_few_serves(const MxArgs& a);
+int64_t mx_few_workspace_bytes(const MxArgs& a);
+hipError_t launch_mx_few(const MxArgs& a, hipStream_t st);
+
 #ifdef __HIPCC__
 typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
 typedef float mx_f32x2 __attribute__((ext_vector_type(2)));

@@ -1,0 +1,483 @@
+// Products of a microscaled matrix with few right-hand sides: one vector (a
+// single token, a gradient step on a vector) up to 64 columns of bf16 values.
+//
+// Bound: reading A's codes once.  The work for a code is a conversion and the
+// matrix instruction, so neither shared memory nor a second copy holds codes:
+// a lane loads the 16 bytes that its own part of a matrix operand is made of,
+// and converts them in registers.  The order in which a sum's terms meet the
+// matrix core is free as long as X is laid out in it, and that decides which
+// bytes a lane loads.
+//
+// Columns: a right-hand side in bf16, or microscaled, is one column of the
+// matrix instruction, an fp32 one is three (split_bf16), plane h of side c at
+// h * s + c.  Lanes of the columns that are left over repeat column 0: a
+// column's sums meet no other column's.
+#include <algorithm>
+
+#include "mx.h"
+
+namespace coded {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kWaves = kThreads / 64;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef u32x4_t u32x4_bf __attribute__((aligned(2)));
+typedef u32x4_t u32x4_f __attribute__((aligned(4)));
+
+// Eight values of a right-hand side, terms k .. k + 7 (zeros from `terms` on),
+// as `planes` times eight bf16.
+__device__ __forceinline__ void load_side(const MxArgs& a, int64_t side, int64_t k, int64_t terms, u32x4_t (&out)[3]) {
+    if (a.x_bits) {
+        uint32_t v[4] = {0u, 0u, 0u, 0u};
+        if (k < terms) {   // past `terms` the codes of the last block are zero
+            const uint8_t* codes = a.XM.codes + side * a.XM.ldc;
+            const uint8_t* scales = a.XM.scales + side * a.XM.lds;
+            if (a.x_bits == 4)
+                mx_eight<4>(codes, scales, k, v);
+            else
+                mx_eight<8>(codes, scales, k, v);
+            if (k + 8 > terms)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (k + i >= terms) v[i / 2] &= i & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+        }
+        out[0] = u32x4_t{v[0], v[1], v[2], v[3]};
+        return;
+    }
+    const int64_t step = a.x_rows ? 1 : a.ldx;
+    const int64_t at = a.x_rows ? side * a.ldx + k : k * a.ldx + side;
+    if (a.x_bf16) {
+        const uint16_t* p = static_cast<const uint16_t*>(a.X) + at;
+        if (a.x_rows && k + 8 <= terms) {
+            out[0] = *reinterpret_cast<const u32x4_bf*>(p);
+        } else {
+            uint32_t v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = k + i < terms ? p[i * step] : 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out[0][i] = v[2 * i] | v[2 * i + 1] << 16;
+        }
+        return;
+    }
+    const float* p = static_cast<const float*>(a.X) + at;
+    float f[8];
+    if (a.x_rows && k + 8 <= terms) {
+        const u32x4_t lo = reinterpret_cast<const u32x4_f*>(p)[0], hi = reinterpret_cast<const u32x4_f*>(p)[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[i] = __uint_as_float(lo[i]);
+            f[4 + i] = __uint_as_float(hi[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = k + i < terms ? p[i * step] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint16_t x[3], y[3];
+        split_bf16(f[2 * i], x);
+        split_bf16(f[2 * i + 1], y);
+#pragma unroll
+        for (int h = 0; h < 3; ++h) out[h][i] = x[h] | static_cast<uint32_t>(y[h]) << 16;
+    }
+}
+
+// Values 8 U .. 8 U + 7 of the 32 of a block as an operand of the matrix instruction.
+template <int BITS, int U>
+__device__ __forceinline__ bf16x8 operand(const u32x4_t* w, float scale) {
+    u32x4_t v;
+    if constexpr (BITS == 4) {
+        const uint32_t c = w[0][U];
+        v = u32x4_t{mx_pair_bf16<4, 0>(c, scale), mx_pair_bf16<4, 1>(c, scale), mx_pair_bf16<4, 2>(c, scale),
+                    mx_pair_bf16<4, 3>(c, scale)};
+    } else {
+        const uint32_t c0 = w[U / 2][2 * (U & 1)], c1 = w[U / 2][2 * (U & 1) + 1];
+        v = u32x4_t{mx_pair_bf16<8, 0>(c0, scale), mx_pair_bf16<8, 1>(c0, scale), mx_pair_bf16<8, 0>(c1, scale),
+                    mx_pair_bf16<8, 1>(c1, scale)};
+    }
+    return __builtin_bit_cast(bf16x8, v);
+}
+
+// ---------------------------------------------------------------- along the blocks
+
+// Y = A X.  A wave takes RT tiles of 16 rows.  Of every kStep terms lane (li,
+// lk) takes row li, blocks SB lk .. SB lk + SB - 1: 64 consecutive bytes of
+// codes and SB consecutive scale bytes; step (t, u) of the matrix instruction
+// takes values 8 u .. of its t-th block.  X lies in shared memory in that order,
+// so each operand is one 16-byte read, contiguous over the wave.  WK of the
+// eight waves share their rows and take every WK-th kStep; their sums are added
+// at the end.  Each kStep's sums start from zero and are added in fp32: a chain
+// of 512 terms, not of all of them.
+//
+// Rows past q and blocks past r repeat the last one: such rows are not stored,
+// and such blocks meet zeros of X (a NaN in the last block is part of its row's
+// sums anyway).
+template <int BITS, int NT, int RT>
+__global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArgs a, int wk_log, int planes, int64_t kc) {
+    constexpr int SB = BITS == 4 ? 4 : 2;          // blocks a lane takes of a step
+    constexpr int V = BITS == 4 ? 1 : 2;           // 16-byte loads of a block
+    constexpr int kStep = 128 * SB;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int WK = 1 << wk_log, wk = wave & (WK - 1), wr = wave >> wk_log;
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * (kWaves >> wk_log) * 16 * RT;
+    const int s = static_cast<int>(a.s), cols = planes * s;
+    const int64_t blocks = ceil_div(a.r, kMxBlock), steps = ceil_div(a.r, kStep);
+
+    const uint8_t *codes[RT], *scales[RT];
+#pragma unroll
+    for (int x = 0; x < RT; ++x) {
+        const int64_t row = min(row0 + (wr * RT + x) * 16 + li, a.q - 1);
+        codes[x] = a.A.codes + row * a.A.ldc;
+        scales[x] = a.A.scales + row * a.A.lds;
+    }
+    u32x4_t w[RT][SB * V];
+    uint32_t sc[RT];
+    const auto fetch = [&](int64_t step) {
+#pragma unroll
+        for (int x = 0; x < RT; ++x) {
+            const int64_t b0 = step * 4 * SB + lk * SB;
+            if (b0 + SB <= blocks) {
+                const u32x4_t* p = reinterpret_cast<const u32x4_t*>(codes[x] + b0 * 16 * V);
+#pragma unroll
+                for (int i = 0; i < SB * V; ++i) w[x][i] = __builtin_nontemporal_load(p + i);
+                sc[x] = SB == 4 ? *reinterpret_cast<const uint32_t*>(scales[x] + b0)
+                                : *reinterpret_cast<const uint16_t*>(scales[x] + b0);
+            } else {
+                sc[x] = 0;
+#pragma unroll
+                for (int t = 0; t < SB; ++t) {
+                    const int64_t b = min(b0 + t, blocks - 1);
+                    const u32x4_t* p = reinterpret_cast<const u32x4_t*>(codes[x] + b * 16 * V);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) w[x][t * V + i] = p[i];
+                    sc[x] |= static_cast<uint32_t>(scales[x][b]) << (8 * t);
+                }
+            }
+        }
+    };
+
+    int col[NT];   // byte offset of this lane's column of a column tile
+#pragma unroll
+    for (int n = 0; n < NT; ++n) col[n] = (16 * n + li < cols ? 16 * n + li : 0) * 16 + lk * cols * 16;
+
+    f32x4_t sum[RT][NT] = {};
+    int64_t mine = wk;   // this wave's next step
+    if (mine < steps) fetch(mine);
+    for (int64_t k0 = 0; k0 < a.r; k0 += kc) {
+        const int64_t end = min(k0 + kc, steps * kStep);
+        __syncthreads();
+        const int groups = static_cast<int>((end - k0) / 8);
+        for (int task = tid; task < groups * s; task += kThreads) {
+            const int g = a.x_rows ? task % groups : task / s, c = a.x_rows ? task / groups : task % s;
+            u32x4_t v[3];
+            load_side(a, c, k0 + g * 8, a.r, v);
+            // group g: term 8 g of the chunk is in step (8 g) / kStep, block b of it, part u of the block
+            const int b = g / 4 % (4 * SB), u = g % 4, st = g / (16 * SB);
+            char* to = smem + (((st * SB + b % SB) * 4 + u) * 4 + b / SB) * cols * 16 + c * 16;
+            for (int h = 0; h < planes; ++h) *reinterpret_cast<u32x4_t*>(to + h * s * 16) = h == 0 ? v[0] : h == 1 ? v[1] : v[2];
+        }
+        __syncthreads();
+        for (; mine * kStep < end; mine += WK) {
+            u32x4_t cw[RT][SB * V];
+            uint32_t cs[RT];
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                cs[x] = sc[x];
+#pragma unroll
+                for (int i = 0; i < SB * V; ++i) cw[x][i] = w[x][i];
+            }
+            if (mine + WK < steps) fetch(mine + WK);
+            const char* xs = smem + static_cast<int>((mine * kStep - k0) / kStep) * (SB * 4 * 4) * cols * 16;
+            f32x4_t acc[RT][NT] = {};
+#pragma unroll
+            for (int t = 0; t < SB; ++t) {
+                float scale[RT];
+#pragma unroll
+                for (int x = 0; x < RT; ++x) scale[x] = mx_scale((cs[x] >> (8 * t)) & 0xFFu);
+                const auto part = [&](auto U) {
+                    bf16x8 xv[NT];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        xv[n] = *reinterpret_cast<const bf16x8*>(xs + (t * 4 + U.value) * 4 * cols * 16 + col[n]);
+#pragma unroll
+                    for (int x = 0; x < RT; ++x) {
+                        const bf16x8 av = operand<BITS, U.value>(&cw[x][t * V], scale[x]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            acc[x][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, xv[n], acc[x][n], 0, 0, 0);
+                    }
+                };
+                part(std::integral_constant<int, 0>{});
+                part(std::integral_constant<int, 1>{});
+                part(std::integral_constant<int, 2>{});
+                part(std::integral_constant<int, 3>{});
+            }
+#pragma unroll
+            for (int x = 0; x < RT; ++x)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) sum[x][n] += acc[x][n];
+        }
+    }
+
+    // the waves' tiles through shared memory: rows x columns each, then the sums over waves and pieces
+    constexpr int kPitch = 16 * NT;
+    float* red = reinterpret_cast<float*>(smem);
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < RT; ++x)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                red[((wk * (kWaves >> wk_log) + wr) * RT * 16 + x * 16 + 4 * lk + v) * kPitch + 16 * n + li] = sum[x][n][v];
+    __syncthreads();
+    const int rows = (kWaves >> wk_log) * RT * 16;
+    for (int task = tid; task < rows * s; task += kThreads) {
+        const int t = a.y_rows ? task % rows : task / s, c = a.y_rows ? task / rows : task % s;
+        if (row0 + t >= a.q) continue;
+        float v = 0.0f;
+        for (int h = 0; h < planes; ++h)
+            for (int k = 0; k < WK; ++k) v += red[(k * rows + t) * kPitch + h * s + c];
+        mx_store(a, c, row0 + t, v);
+    }
+}
+
+// ---------------------------------------------------------------- across the blocks
+
+// Z = A^T U.  A wave takes W bytes of 16 neighbouring lanes' columns and walks
+// down the rows, 32 a step: lane (li, lk) loads W bytes of rows 8 lk .. 8 lk +
+// 7, which is an 8 x CW piece of A with all the terms that the matrix operand
+// of each of its CW columns needs of this lane: result tile n is column n of
+// every lane's piece.  The conversion makes pairs along a row and the operand
+// takes pairs down a column, so two rows' pairs are exchanged by two byte
+// permutations.
+//
+// The eight waves of a workgroup take every eighth step, workgroups take
+// `per` rows each; a wave's sums go through shared memory to the workgroup's,
+// and those of several workgroups to `part` (workgroup, side, column), which
+// mx_join_kernel adds up in order.
+//
+// Rows past q repeat the last one and meet zeros of U; columns past r repeat
+// the last block and are not stored.
+template <int BITS, int W>
+__global__ __launch_bounds__(kThreads, 2) void mx_few_t_kernel(MxArgs a, int planes, int64_t per, int rows_staged, int64_t groups,
+                                                               float* part) {
+    constexpr int CW = W * 8 / BITS;   // columns of a lane
+    constexpr int kCols = 16 * CW;     // and of a workgroup
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t group = blockIdx.x % groups, split = blockIdx.x / groups;
+    const int64_t t0 = split * per, t1 = min(t0 + per, a.q);
+    const int s = static_cast<int>(a.s), cols = planes * s;
+    const int64_t j0 = group * kCols;
+    // this lane's columns, moved back to the last whole piece
+    const int64_t j = min(j0 + li * CW, ceil_div(a.r, kMxBlock) * kMxBlock - CW);
+    const uint8_t* codes = a.A.codes + j * BITS / 8;
+    const uint8_t* scales = a.A.scales + j / kMxBlock;
+    typedef unsigned int words_t __attribute__((ext_vector_type(W / 4)));
+    words_t w[8];
+    uint32_t sc[8];
+    const auto fetch = [&](int64_t t) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int64_t row = min(t + 8 * lk + e, a.q - 1);
+            w[e] = __builtin_nontemporal_load(reinterpret_cast<const words_t*>(codes + row * a.A.ldc));
+            sc[e] = scales[row * a.A.lds];
+        }
+    };
+    f32x4_t acc[CW] = {};
+    const int col = (li < cols ? li : 0) * 16 + lk * cols * 16;
+    int64_t mine = t0 + wave * 32;
+    if (mine < t1) fetch(mine);
+    for (int64_t c0 = t0; c0 < t1; c0 += rows_staged) {
+        const int64_t end = min(c0 + rows_staged, t1);
+        __syncthreads();
+        const int pieces = static_cast<int>(ceil_div(end - c0, 32)) * 4;
+        for (int task = tid; task < pieces * s; task += kThreads) {
+            const int g = a.x_rows ? task % pieces : task / s, c = a.x_rows ? task / pieces : task % s;
+            u32x4_t v[3];
+            load_side(a, c, c0 + g * 8, t1, v);
+            char* to = smem + (g * cols + c) * 16;
+            for (int h = 0; h < planes; ++h) *reinterpret_cast<u32x4_t*>(to + h * s * 16) = h == 0 ? v[0] : h == 1 ? v[1] : v[2];
+        }
+        __syncthreads();
+        for (; mine < end; mine += 32 * kWaves) {
+            const bf16x8 u = *reinterpret_cast<const bf16x8*>(smem + static_cast<int>(mine - c0) / 8 * cols * 16 + col);
+            words_t cw[8];
+            float scale[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                cw[e] = w[e];
+                scale[e] = mx_scale(sc[e]);
+            }
+            if (mine + 32 * kWaves < t1) fetch(mine + 32 * kWaves);
+            // a word holds 8 (4) columns: pairs of them, then down the rows
+            const auto pair = [&](auto P, int word) {
+                uint32_t v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = mx_pair_bf16<BITS, P.value>(cw[e][word], scale[e]);
+                u32x4_t even, odd;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    even[e] = __builtin_amdgcn_perm(v[2 * e + 1], v[2 * e], 0x05040100u);
+                    odd[e] = __builtin_amdgcn_perm(v[2 * e + 1], v[2 * e], 0x07060302u);
+                }
+                const int n = word * (32 / BITS) + 2 * P.value;
+                acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, __builtin_bit_cast(bf16x8, even), acc[n], 0, 0, 0);
+                acc[n + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, __builtin_bit_cast(bf16x8, odd), acc[n + 1], 0, 0, 0);
+            };
+#pragma unroll
+            for (int word = 0; word < W / 4; ++word) {
+                pair(std::integral_constant<int, 0>{}, word);
+                pair(std::integral_constant<int, 1>{}, word);
+                if constexpr (BITS == 4) {
+                    pair(std::integral_constant<int, 2>{}, word);
+                    pair(std::integral_constant<int, 3>{}, word);
+                }
+            }
+        }
+    }
+    // acc[n][v]: side 4 lk + v (of `cols`), column j0 + li CW + n.  One wave after
+    // another would be a chain of barriers; four columns of every lane at a time
+    // keep the waves' tiles within 64 x 65 floats each.
+    float* red = reinterpret_cast<float*>(smem);
+    constexpr int kPass = 4;          // columns of a lane a pass
+    constexpr int kPitch = 16 * kPass + 1;
+#pragma unroll
+    for (int n0 = 0; n0 < CW; n0 += kPass) {
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kPass; ++n)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                if (4 * lk + v < cols) red[(wave * cols + 4 * lk + v) * kPitch + li * kPass + n] = acc[n0 + n][v];
+        __syncthreads();
+        for (int task = tid; task < 16 * kPass * s; task += kThreads) {
+            const int p = task % (16 * kPass), c = task / (16 * kPass);
+            const int64_t at = j0 + p / kPass * CW + n0 + p % kPass;
+            if (at >= a.r) continue;
+            float v = 0.0f;
+            for (int h = 0; h < planes; ++h)
+#pragma unroll
+                for (int k = 0; k < kWaves; ++k) v += red[(k * cols + h * s + c) * kPitch + p];
+            if (part)
+                part[(split * s + c) * a.r + at] = v;
+            else
+                mx_store(a, c, at, v);
+        }
+    }
+}
+
+// Y from the partial sums of `splits` workgroups, part[split][side][result], in order.
+__global__ __launch_bounds__(256) void mx_join_kernel(MxArgs a, const float* part, int64_t splits, int64_t n) {
+    // a workgroup takes 32 results of one side; eight threads share each of them
+    __shared__ float red[8][33];
+    const int64_t tiles = ceil_div(n, 32);
+    const int64_t side = blockIdx.x / tiles, at = blockIdx.x % tiles * 32 + (threadIdx.x & 31);
+    const int g = threadIdx.x >> 5;
+    float v = 0.0f;
+    if (at < n)
+        for (int64_t p = g; p < splits; p += 8) v += part[(p * a.s + side) * n + at];
+    red[g][threadIdx.x & 31] = v;
+    __syncthreads();
+    if (g == 0 && at < n) {
+#pragma unroll
+        for (int i = 1; i < 8; ++i) v += red[i][threadIdx.x & 31];
+        mx_store(a, side, at, v);
+    }
+}
+
+int planes_of(const MxArgs& a) { return a.x_bits || a.x_bf16 ? 1 : 3; }
+
+constexpr int64_t kXBytes = 64 << 10;   // of X in shared memory: two workgroups a compute unit
+
+template <int BITS, int NT, int RT>
+hipError_t launch_few(const MxArgs& a, hipStream_t st) {
+    constexpr int64_t kStep = BITS == 4 ? 512 : 256;
+    const int planes = planes_of(a);
+    const int64_t cols = planes * a.s, steps = ceil_div(a.r, kStep);
+    // Waves on the same rows: as many as make 2048 of them, as X's share of shared memory holds a step for
+    // each, and as there are steps.
+    int wk_log = 0;
+    const int64_t tiles = ceil_div(a.q, 16 * RT);
+    while (wk_log < 3 && (tiles << wk_log) < 2048 && (int64_t(2) << wk_log) * kStep * cols * 2 <= kXBytes &&
+           (int64_t(2) << wk_log) <= steps)
+        ++wk_log;
+    const int64_t unit = kStep << wk_log;
+    const int64_t kc = std::max<int64_t>(1, std::min(kXBytes / (cols * 2) / unit, ceil_div(a.r, unit))) * unit;
+    const int64_t blocks = ceil_div(a.q, (kWaves >> wk_log) * 16 * RT);
+    if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
+    const int64_t x_bytes = std::min(kc, steps * kStep) * cols * 2, red_bytes = kWaves * 16 * RT * 16 * NT * 4;
+    mx_few_kernel<BITS, NT, RT><<<dim3(static_cast<uint32_t>(blocks)), kThreads, std::max(x_bytes, red_bytes), st>>>(
+        a, wk_log, planes, kc);
+    return hipGetLastError();
+}
+
+template <int BITS>
+hipError_t launch_few_cols(const MxArgs& a, hipStream_t st) {
+    const int64_t cols = planes_of(a) * a.s;
+    if (cols <= 16) return launch_few<BITS, 1, 1>(a, st);
+    if (cols <= 32) return launch_few<BITS, 2, 2>(a, st);
+    return launch_few<BITS, 4, 2>(a, st);
+}
+
+// Workgroups that share the columns of mx_few_t_kernel: about 512 in all, each
+// with at least two steps for each of its waves.
+constexpr int kTBytes = 16;
+int64_t t_groups(const MxArgs& a) { return ceil_div(a.r, 16 * kTBytes * 8 / a.A.bits); }
+int64_t t_rows(const MxArgs& a) {
+    const int64_t splits = std::max<int64_t>(1, 512 / t_groups(a));
+    const int64_t unit = 32 * kWaves;
+    return std::max<int64_t>(2, ceil_div(ceil_div(a.q, splits), unit)) * unit;
+}
+
+template <int BITS>
+hipError_t launch_few_t(const MxArgs& a, hipStream_t st) {
+    const int planes = planes_of(a);
+    const int64_t cols = planes * a.s, groups = t_groups(a), per = t_rows(a), splits = std::max<int64_t>(1, ceil_div(a.q, per));
+    const int64_t unit = 32 * kWaves;
+    const int64_t staged = std::min(per, std::max<int64_t>(1, (32 << 10) / (cols * 2) / unit) * unit);
+    if (!grid_fits(groups * splits, kThreads)) return hipErrorInvalidConfiguration;
+    constexpr int kPitch = 16 * 4 + 1;
+    const int64_t lds = std::max<int64_t>(staged * cols * 2, kWaves * cols * kPitch * 4);
+    float* part = splits > 1 ? static_cast<float*>(a.workspace) : nullptr;
+    mx_few_t_kernel<BITS, kTBytes><<<dim3(static_cast<uint32_t>(groups * splits)), kThreads, lds, st>>>(
+        a, planes, per, static_cast<int>(staged), groups, part);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !part) return e;
+    const int64_t blocks = ceil_div(a.r, 32) * a.s;
+    if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+    mx_join_kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a, part, splits, a.r);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+bool mx_few_serves(const MxArgs& a) {
+    const int64_t terms = a.trans ? a.q : a.r;
+    return terms > 0 && a.s <= 64 && planes_of(a) * a.s <= (a.trans ? 16 : 64);
+}
+
+int64_t mx_few_workspace_bytes(const MxArgs& a) {
+    if (!a.trans) return 0;
+    const int64_t splits = ceil_div(a.q, t_rows(a));
+    return splits > 1 ? splits * a.s * a.r * 4 : 0;
+}
+
+hipError_t launch_mx_few(const MxArgs& args, hipStream_t st) {
+    MxArgs a = args;
+    if (a.s == 1 && !a.x_rows && a.ldx == 1) {   // one contiguous right-hand side
+        a.x_rows = 1;
+        a.ldx = a.trans ? a.q : a.r;
+    }
+    if (a.trans) return a.A.bits == 4 ? launch_few_t<4>(a, st) : launch_few_t<8>(a, st);
+    return a.A.bits == 4 ? launch_few_cols<4>(a, st) : launch_few_cols<8>(a, st);
+}
+
+}  // namespace coded
