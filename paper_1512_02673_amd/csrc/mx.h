@@ -54,6 +54,13 @@ bool mx_few_serves(const MxArgs& a);
 int64_t mx_few_workspace_bytes(const MxArgs& a);
 hipError_t launch_mx_few(const MxArgs& a, hipStream_t st);
 
+// Many dense ones (mx_tiled.hip).
+bool mx_tiled_serves(const MxArgs& a);
+int64_t mx_tiled_workspace_bytes(const MxArgs& a);
+hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st);
+// Y from partial sums part[split][side][result] of n results a side, added in order.
+hipError_t launch_mx_join(const MxArgs& a, const float* part, int64_t splits, int64_t n, hipStream_t st);
+
 #ifdef __HIPCC__
 typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
 typedef float mx_f32x2 __attribute__((ext_vector_type(2)));

@@ -451,13 +451,17 @@ hipError_t launch_few_t(const MxArgs& a, hipStream_t st) {
         a, planes, per, static_cast<int>(staged), groups, part);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !part) return e;
-    const int64_t blocks = ceil_div(a.r, 32) * a.s;
-    if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
-    mx_join_kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a, part, splits, a.r);
-    return hipGetLastError();
+    return launch_mx_join(a, part, splits, a.r, st);
 }
 
 }  // namespace
+
+hipError_t launch_mx_join(const MxArgs& a, const float* part, int64_t splits, int64_t n, hipStream_t st) {
+    const int64_t blocks = ceil_div(n, 32) * a.s;
+    if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+    mx_join_kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a, part, splits, n);
+    return hipGetLastError();
+}
 
 bool mx_few_serves(const MxArgs& a) {
     const int64_t terms = a.trans ? a.q : a.r;

@@ -1,0 +1,433 @@
+// Products of a microscaled matrix with many dense right-hand sides, on the
+// bf16 matrix cores: out[i][j] = sum over k of P[i][k] Q[j][k], i a right-hand
+// side, j a result, Q the codes' values (exact in bf16).
+//
+// P is X in bf16 with k contiguous, rows of whole steps and 16-byte aligned: X
+// itself where it is that already, else a copy that mx_pack_kernel lays out in
+// the workspace (transposed, padded with zeros, an fp32 X as three planes,
+// split_bf16, that are summed one after the other).  Terms past the last one
+// meet those zeros, so A's operands need no masks there, only finite values:
+// rows and blocks past the end repeat the last one, whose own NaN would be in
+// the same sums.
+//
+// Bound: the matrix cores.  Four waves share a tile of 64 to 128 right-hand
+// sides and 128 to 256 results; two such workgroups on a compute unit cover
+// each other's barriers.  A step's operands come from memory into registers
+// while the step before is computed, then into shared memory.
+#include <algorithm>
+
+#include "mx.h"
+
+namespace coded {
+namespace {
+
+constexpr int kThreads = 256;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef f32x4_t f32x4_any __attribute__((aligned(4)));
+typedef u32x2_t u32x2_any __attribute__((aligned(2)));
+
+constexpr int kStep = 64;   // terms
+
+// Loads within `bytes` of `base`; past them they give zeros.
+struct Window {
+    __amdgpu_buffer_rsrc_t rsrc;
+    __device__ __forceinline__ Window(const void* base, int64_t bytes)
+        : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, static_cast<int>(min<int64_t>(max<int64_t>(bytes, 0), 0xFFFFFFFF)),
+                                                 0x00027000)) {}
+    __device__ __forceinline__ u32x4_t four(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0); }
+    __device__ __forceinline__ uint32_t two_bytes(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0); }
+    __device__ __forceinline__ uint32_t byte(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b8(rsrc, at, 0, 0); }
+};
+
+struct TileArgs {
+    const uint16_t* P;
+    int64_t pitch, plane;       // elements between rows, and between planes
+    int64_t row;                // elements of a row that are there: whole steps
+    int32_t planes;
+    int64_t steps;              // of one plane
+    int64_t per;                // steps of a split
+    int64_t splits;
+    float* part;                // sums of each split [split][side][result], or null
+    int64_t tiles_i, tiles_j;
+    int32_t flush;              // steps summed in one chain (fp32 results), 0: all
+};
+
+// A result's tile of four: results j .. j + 3 of side i (YROWS), or result j of sides i .. i + 3.
+template <bool YROWS>
+__device__ __forceinline__ void store_four(const MxArgs& a, float* part, int64_t n, int64_t i, int64_t j, f32x4_t v, bool first) {
+    const int64_t side = i, have = YROWS ? n - j : a.s - i;
+    if (have <= 0 || (YROWS ? i >= a.s : j >= n)) return;
+    if (part) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < have) part[YROWS ? side * n + j + e : (side + e) * n + j] = v[e];
+        return;
+    }
+    const int64_t at = YROWS ? i * a.ldy + j : j * a.ldy + i, ct = YROWS ? i * a.ldcc + j : j * a.ldcc + i;
+    v *= a.alpha;
+    if (a.C && first) {
+        float c[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (a.y_bf16)
+                c[e] = e < have ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(a.C)[ct + e]) << 16) : 0.f;
+            else
+                c[e] = e < have ? static_cast<const float*>(a.C)[ct + e] : 0.f;
+            v[e] = fmaf(a.beta, c[e], v[e]);
+        }
+    }
+    if (a.y_bf16) {
+        uint16_t* y = static_cast<uint16_t*>(a.Y) + at;
+        uint16_t b[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] = mx_to_bf16(v[e]);
+        if (have >= 4) {
+            *reinterpret_cast<u32x2_any*>(y) = u32x2_t{b[0] | static_cast<uint32_t>(b[1]) << 16, b[2] | static_cast<uint32_t>(b[3]) << 16};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (e < have) y[e] = b[e];
+        }
+    } else {
+        float* y = static_cast<float*>(a.Y) + at;
+        if (have >= 4) {
+            if (!first) v += *reinterpret_cast<const f32x4_any*>(y);
+            *reinterpret_cast<f32x4_any*>(y) = v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (e < have) y[e] = first ? v[e] : y[e] + v[e];
+        }
+    }
+}
+
+// Two waves along each side of the tile, each of TI x TJ tiles of 16 x 16.
+//
+// Along the blocks (mm): shared memory holds codes, and each wave converts its
+// operands.  Lane (li, lk) of a step's 64 terms takes 16 lk .. 16 lk + 15, eight
+// for each of two matrix instructions.  Across them (mm_t): the conversion
+// comes before shared memory, which holds rows of bf16 values; the operands,
+// eight terms of a column, are read transposed.  Lane (li, lk) takes terms 8 lk
+// .. 8 lk + 7 of each 32.
+template <int BITS, bool TRANS, int TI, int TJ, bool YROWS>
+__global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs g) {
+    constexpr int BI = 32 * TI, BJ = 32 * TJ;
+    constexpr int kPRow = kStep * 2, kPChunks = kPRow / 16;          // bytes and 16-byte pieces of a row of P
+    constexpr int kPLoads = BI * kPChunks / kThreads;
+    constexpr int kQRow = TRANS ? BJ * 2 : kStep * BITS / 8;         // shared memory: [k][j] in bf16, or [j] codes
+    constexpr int kQRows = TRANS ? kStep : BJ;
+    constexpr int kQPieces = TRANS ? BJ * BITS / 8 / 16 : kQRow / 16;   // 16-byte pieces of codes in a row of the tile
+    constexpr int kQLoads = kQRows * kQPieces / kThreads;
+    constexpr int kSLoads = TRANS ? kQLoads : 1;
+    __shared__ __attribute__((aligned(16))) char Ps[BI * kPRow];
+    __shared__ __attribute__((aligned(16))) char Qs[kQRows * kQRow];
+    __shared__ uint32_t Ss[TRANS ? 1 : BJ];
+    static_assert(kQLoads >= 1 && kQRows * kQPieces % kThreads == 0, "codes must split evenly over the threads");
+
+    const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wi = (wave & 1) * TI * 16, wj = (wave >> 1) * TJ * 16;
+    const int64_t n = TRANS ? a.r : a.q;
+    const int64_t blocks = ceil_div(a.r, kMxBlock), code_row = blocks * 4 * BITS;
+
+    // Workgroups go to the eight XCDs in turn: each takes a run of tiles of its own, in strips of 8 tiles of
+    // right-hand sides, so that what its L2 holds is used by several of them.
+    const int64_t total = g.tiles_i * g.tiles_j;
+    int64_t id = blockIdx.x % total;
+    const int64_t split = blockIdx.x / total;
+    {
+        const int64_t base = total / 8, rest = total % 8, x = id % 8, y = id / 8;
+        id = x * base + min(x, rest) + y;
+    }
+    const int64_t strip = id / (8 * g.tiles_j), in = id % (8 * g.tiles_j), high = min<int64_t>(8, g.tiles_i - strip * 8);
+    const int64_t i0 = (strip * 8 + in % high) * BI, j0 = in / high * BJ;
+
+    // what this thread loads of a step: byte offsets in the tile's rows
+    const uint32_t p_at = static_cast<uint32_t>(tid / kPChunks * g.pitch * 2 + tid % kPChunks * 16);
+    const uint32_t q_at = static_cast<uint32_t>(tid / kQPieces * a.A.ldc + tid % kQPieces * 16);
+    const uint32_t s_at = static_cast<uint32_t>(TRANS ? tid / kQPieces * a.A.lds + tid % kQPieces * 4 / BITS : min(tid, BJ - 1) * a.A.lds);
+    u32x4_t p_next[kPLoads], q_next[kQLoads];
+    uint32_t s_next[kSLoads];
+    const auto fetch = [&](int64_t t) {
+        const int64_t h = t / g.steps, k0 = (t - h * g.steps) * kStep;
+        const Window p(g.P + h * g.plane + i0 * g.pitch + k0, ((a.s - i0 - 1) * g.pitch + g.row - k0) * 2);
+#pragma unroll
+        for (int l = 0; l < kPLoads; ++l) p_next[l] = p.four(p_at + static_cast<uint32_t>(l * (kThreads / kPChunks) * 2 * g.pitch));
+        if constexpr (TRANS) {
+            // rows past q are zeros; columns past r are other bytes within A, and are not stored
+            const int64_t c0 = j0 * BITS / 8, b0 = j0 / kMxBlock;
+            const Window q(a.A.codes + k0 * a.A.ldc + c0, (a.q - k0 - 1) * a.A.ldc + code_row - c0);
+            const Window s(a.A.scales + k0 * a.A.lds + b0, (a.q - k0 - 1) * a.A.lds + blocks - b0);
+#pragma unroll
+            for (int l = 0; l < kQLoads; ++l) {
+                q_next[l] = q.four(q_at + static_cast<uint32_t>(l * (kThreads / kQPieces) * a.A.ldc));
+                s_next[l] = s.byte(s_at + static_cast<uint32_t>(l * (kThreads / kQPieces) * a.A.lds));
+            }
+        } else {
+            const int64_t c0 = k0 * BITS / 8, b0 = k0 / kMxBlock;
+            const Window q(a.A.codes + j0 * a.A.ldc + c0, (a.q - j0 - 1) * a.A.ldc + code_row - c0);
+            const Window s(a.A.scales + j0 * a.A.lds + b0, (a.q - j0 - 1) * a.A.lds + ceil_div(blocks, 4) * 4 - b0);
+#pragma unroll
+            for (int l = 0; l < kQLoads; ++l) q_next[l] = q.four(q_at + static_cast<uint32_t>(l * (kThreads / kQPieces) * a.A.ldc));
+            s_next[0] = s.two_bytes(s_at);
+            if (k0 + kStep > blocks * kMxBlock) {   // one block left: what lies behind a row is not a number for sure
+                s_next[0] &= 0xFFu;
+                if (tid % kQPieces >= kQPieces / 2)
+#pragma unroll
+                    for (int l = 0; l < kQLoads; ++l) q_next[l] = u32x4_t{0u, 0u, 0u, 0u};
+            }
+        }
+    };
+    const auto stage = [&] {
+#pragma unroll
+        for (int l = 0; l < kPLoads; ++l) {
+            const int id_ = tid + l * kThreads, row = id_ / kPChunks, c = id_ % kPChunks;
+            *reinterpret_cast<u32x4_t*>(Ps + row * kPRow + (c ^ ((row >> 1) & 7)) * 16) = p_next[l];
+        }
+#pragma unroll
+        for (int l = 0; l < kQLoads; ++l) {
+            const int id_ = tid + l * kThreads, row = id_ / kQPieces, c = id_ % kQPieces;
+            char* to = Qs + row * kQRow;
+            if constexpr (!TRANS) {
+                const int at = BITS == 4 ? c ^ ((row >> 3) & 1) : (c + (row >> 2)) & 3;
+                *reinterpret_cast<u32x4_t*>(to + at * 16) = q_next[l];
+            } else {
+                const float s = mx_scale(s_next[l]);
+                const int f = BJ >= 128 ? (row & 3) | ((row >> 1) & 4) : ((row >> 1) & 1) | ((row >> 2) & 2);
+#pragma unroll
+                for (int e = 0; e < 16 / BITS; ++e) {
+                    u32x4_t v;
+                    if constexpr (BITS == 4) {
+                        const uint32_t w = q_next[l][e];
+                        v = u32x4_t{mx_pair_bf16<4, 0>(w, s), mx_pair_bf16<4, 1>(w, s), mx_pair_bf16<4, 2>(w, s), mx_pair_bf16<4, 3>(w, s)};
+                    } else {
+                        const uint32_t w0 = q_next[l][2 * e], w1 = q_next[l][2 * e + 1];
+                        v = u32x4_t{mx_pair_bf16<8, 0>(w0, s), mx_pair_bf16<8, 1>(w0, s), mx_pair_bf16<8, 0>(w1, s), mx_pair_bf16<8, 1>(w1, s)};
+                    }
+                    *reinterpret_cast<u32x4_t*>(to + ((c * (8 / BITS) + e / 2) ^ f) * 32 + (e & 1) * 16) = v;
+                }
+            }
+        }
+        if constexpr (!TRANS)
+            if (tid < BJ) Ss[tid] = s_next[0];
+    };
+
+    f32x4_t acc[TI][TJ] = {};
+    const auto compute = [&] {
+        [[maybe_unused]] float scale[TJ];
+        [[maybe_unused]] u32x4_t code[TJ];
+        if constexpr (!TRANS) {
+#pragma unroll
+            for (int y = 0; y < TJ; ++y) {
+                const int row = wj + 16 * y + li;
+                scale[y] = mx_scale((Ss[row] >> (8 * (lk >> 1))) & 0xFFu);
+                if constexpr (BITS == 4) {
+                    const u32x2_t c = *reinterpret_cast<const u32x2_t*>(Qs + row * kQRow + ((lk >> 1) ^ ((row >> 3) & 1)) * 16 + (lk & 1) * 8);
+                    code[y] = u32x4_t{c[0], c[1], 0u, 0u};
+                } else {
+                    code[y] = *reinterpret_cast<const u32x4_t*>(Qs + row * kQRow + ((lk + (row >> 2)) & 3) * 16);
+                }
+            }
+        }
+        const int f = BJ >= 128 ? ((li >> 2) & 3) | ((lk & 1) << 2) : ((li >> 3) & 1) | ((lk & 1) << 1);
+        const char* qrow = Qs + (8 * lk + (li >> 2)) * kQRow + (li & 3) * 8;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            bf16x8 pv[TI];
+#pragma unroll
+            for (int x = 0; x < TI; ++x) {
+                const int row = wi + 16 * x + li, c = TRANS ? 4 * u + lk : 2 * lk + u;
+                pv[x] = *reinterpret_cast<const bf16x8*>(Ps + row * kPRow + (c ^ ((row >> 1) & 7)) * 16);
+            }
+#pragma unroll
+            for (int y = 0; y < TJ; ++y) {
+                bf16x8 qv;
+                if constexpr (TRANS) {
+                    typedef __attribute__((address_space(3))) s16x4_t lds4;
+                    const char* at = qrow + 32 * u * kQRow + ((wj / 16 + y) ^ f) * 32;
+                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(at));
+                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(at + 4 * kQRow));
+                    qv = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                } else {
+                    u32x4_t d;
+                    if constexpr (BITS == 4) {
+                        const uint32_t c = code[y][u];
+                        d = u32x4_t{mx_pair_bf16<4, 0>(c, scale[y]), mx_pair_bf16<4, 1>(c, scale[y]), mx_pair_bf16<4, 2>(c, scale[y]),
+                                    mx_pair_bf16<4, 3>(c, scale[y])};
+                    } else {
+                        const uint32_t c0 = code[y][2 * u], c1 = code[y][2 * u + 1];
+                        d = u32x4_t{mx_pair_bf16<8, 0>(c0, scale[y]), mx_pair_bf16<8, 1>(c0, scale[y]), mx_pair_bf16<8, 0>(c1, scale[y]),
+                                    mx_pair_bf16<8, 1>(c1, scale[y])};
+                    }
+                    qv = __builtin_bit_cast(bf16x8, d);
+                }
+#pragma unroll
+                for (int x = 0; x < TI; ++x)
+                    acc[x][y] = YROWS ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(qv, pv[x], acc[x][y], 0, 0, 0)
+                                      : __builtin_amdgcn_mfma_f32_16x16x32_bf16(pv[x], qv, acc[x][y], 0, 0, 0);
+            }
+        }
+    };
+    float* part = g.part ? g.part + split * a.s * n : nullptr;
+    // the lane's place in the tile, computed anew each time: kept, its addresses would take registers from the sums
+    const auto put = [&](bool first) {
+        int at = tid;
+        asm volatile("" : "+v"(at));
+        const int l15 = at & 15, l4 = (at >> 4 & 3) * 4;
+#pragma unroll
+        for (int x = 0; x < TI; ++x)
+#pragma unroll
+            for (int y = 0; y < TJ; ++y) {
+                const int64_t i = i0 + wi + 16 * x + (YROWS ? l15 : l4), j = j0 + wj + 16 * y + (YROWS ? l4 : l15);
+                store_four<YROWS>(a, part, n, i, j, acc[x][y], first);
+                acc[x][y] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            }
+    };
+
+    int64_t t = split * g.per;
+    const int64_t t1 = min(t + g.per, g.steps * g.planes);
+    if (t < t1) {
+        fetch(t);
+        stage();
+    }
+    for (bool first = true;; first = false) {
+        const int64_t end = g.flush ? min(t + g.flush, t1) : t1;
+        for (; t < end; ++t) {
+            __syncthreads();
+            if (t + 1 < t1) fetch(t + 1);
+            compute();
+            __syncthreads();
+            if (t + 1 < t1) stage();
+        }
+        put(first);
+        if (t >= t1) break;
+    }
+}
+
+// X in bf16, k contiguous: to[plane][side][pitch], zeros from `terms` on.  A workgroup takes 64 sides x 64 terms.
+template <bool BF16>
+__global__ __launch_bounds__(256) void mx_pack_kernel(const void* X, int64_t ldx, int32_t x_rows, int64_t s, int64_t terms, uint16_t* to,
+                                                      int64_t pitch, int64_t plane) {
+    constexpr int PL = BF16 ? 1 : 3;
+    __shared__ uint16_t tile[PL][64][66];
+    const int64_t strips = ceil_div(pitch, 64);
+    const int64_t k0 = blockIdx.x % strips * 64, i0 = blockIdx.x / strips * 64;
+    const int lo = threadIdx.x & 63, hi = threadIdx.x >> 6;
+    for (int e = 0; e < 16; ++e) {
+        // consecutive threads on consecutive elements of X
+        const int ti = x_rows ? hi + 4 * e : lo, tk = x_rows ? lo : hi + 4 * e;
+        const int64_t i = i0 + ti, k = k0 + tk;
+        const bool in = i < s && k < terms;
+        const int64_t at = x_rows ? i * ldx + k : k * ldx + i;
+        if constexpr (BF16) {
+            tile[0][ti][tk] = in ? static_cast<const uint16_t*>(X)[at] : 0;
+        } else {
+            uint16_t p[3];
+            split_bf16(in ? static_cast<const float*>(X)[at] : 0.0f, p);
+#pragma unroll
+            for (int h = 0; h < 3; ++h) tile[h][ti][tk] = p[h];
+        }
+    }
+    __syncthreads();
+    for (int e = 0; e < 16; ++e) {
+        const int64_t i = i0 + hi + 4 * e, k = k0 + lo;
+        if (i < s && k < pitch)
+#pragma unroll
+            for (int h = 0; h < PL; ++h) to[h * plane + i * pitch + k] = tile[h][hi + 4 * e][lo];
+    }
+}
+
+// How a product is cut up.
+struct Plan {
+    bool pack;          // X goes through the workspace
+    int planes;
+    int64_t steps, pitch, plane, pack_bytes;
+    bool large;         // tiles of 128 x 256, else 64 x 128
+    int64_t tiles_i, tiles_j, per, splits;
+    int64_t part_bytes;
+};
+
+constexpr int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
+
+// x: X and its stride are known (a launch); else the workspace is sized for an X that has to be packed.
+Plan make_plan(const MxArgs& a, bool x) {
+    Plan p{};
+    const int64_t terms = a.trans ? a.q : a.r, n = a.trans ? a.r : a.q;
+    p.planes = a.x_bf16 ? 1 : 3;
+    p.steps = ceil_div(terms, kStep);
+    p.pitch = p.steps * kStep;
+    p.plane = a.s * p.pitch;
+    p.pack = !(x && a.x_bf16 && a.x_rows && terms % kStep == 0 && a.ldx % 8 == 0 && (reinterpret_cast<uintptr_t>(a.X) & 15) == 0);
+    p.pack_bytes = round_up(p.planes * p.plane * 2, 256);
+    const int64_t wide = ceil_div(a.s, 128) * ceil_div(n, 256);
+    p.large = wide >= 256;
+    p.tiles_i = ceil_div(a.s, p.large ? 128 : 64);
+    p.tiles_j = ceil_div(n, p.large ? 256 : 128);
+    const int64_t steps = p.steps * p.planes;
+    p.splits = p.large ? 1 : std::max<int64_t>(1, std::min(512 / (p.tiles_i * p.tiles_j), steps / 4));
+    p.per = std::max<int64_t>(1, ceil_div(steps, p.splits));
+    p.splits = std::max<int64_t>(1, ceil_div(steps, p.per));
+    p.part_bytes = p.splits > 1 ? p.splits * a.s * n * 4 : 0;
+    return p;
+}
+
+template <int BITS, bool TRANS>
+hipError_t launch_tiles(const MxArgs& a, const TileArgs& g, bool large, hipStream_t st) {
+    const dim3 grid(static_cast<uint32_t>(g.tiles_i * g.tiles_j * g.splits));
+    // split sums are laid out as y_rows results are
+    const auto kernel = large ? (a.y_rows ? mx_tile_kernel<BITS, TRANS, 4, 8, true> : mx_tile_kernel<BITS, TRANS, 4, 8, false>)
+                              : (a.y_rows ? mx_tile_kernel<BITS, TRANS, 2, 4, true> : mx_tile_kernel<BITS, TRANS, 2, 4, false>);
+    kernel<<<grid, kThreads, 0, st>>>(a, g);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Offsets within a tile's rows, of X and of codes, are 32-bit.
+bool mx_tiled_serves(const MxArgs& a) {
+    const int64_t most = (int64_t(1) << 31) / 256;
+    return !a.x_bits && (a.trans ? a.q : a.r) < most / 2 && std::max(a.A.ldc, a.A.lds) < most && (!a.x_rows || a.ldx < most / 2);
+}
+
+int64_t mx_tiled_workspace_bytes(const MxArgs& a) {
+    const Plan p = make_plan(a, false);
+    return p.pack_bytes + p.part_bytes;
+}
+
+hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
+    const Plan p = make_plan(a, true);
+    const int64_t n = a.trans ? a.r : a.q, terms = a.trans ? a.q : a.r;
+    TileArgs g{};
+    g.P = p.pack ? static_cast<const uint16_t*>(a.workspace) : static_cast<const uint16_t*>(a.X);
+    g.pitch = p.pack ? p.pitch : a.ldx;
+    g.plane = p.plane;
+    g.row = p.pitch;
+    g.planes = p.planes;
+    g.steps = p.steps;
+    g.per = p.per;
+    g.splits = p.splits;
+    g.part = p.splits > 1 ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + p.pack_bytes) : nullptr;
+    g.tiles_i = p.tiles_i;
+    g.tiles_j = p.tiles_j;
+    g.flush = a.y_bf16 || g.part ? 0 : 8192 / kStep;
+    if (!grid_fits(p.tiles_i * p.tiles_j * p.splits, kThreads)) return hipErrorInvalidConfiguration;
+    if (p.pack && p.pitch > 0) {
+        const int64_t blocks = ceil_div(p.pitch, 64) * ceil_div(a.s, 64);
+        if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+        const auto kernel = a.x_bf16 ? mx_pack_kernel<true> : mx_pack_kernel<false>;
+        kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a.X, a.ldx, a.x_rows, a.s, terms,
+                                                                    static_cast<uint16_t*>(a.workspace), p.pitch, p.plane);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const hipError_t e = a.A.bits == 4 ? (a.trans ? launch_tiles<4, true>(a, g, p.large, st) : launch_tiles<4, false>(a, g, p.large, st))
+                                       : (a.trans ? launch_tiles<8, true>(a, g, p.large, st) : launch_tiles<8, false>(a, g, p.large, st));
+    if (e != hipSuccess || !g.part) return e;
+    return launch_mx_join(a, g.part, g.splits, n, st);
+}
+
+}  // namespace coded
