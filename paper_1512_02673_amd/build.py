@@ -20,7 +20,7 @@ ARCH = "gfx950"
 
 SOURCES = ["api.cpp", "mx_api.cpp", "survivors.cpp", "shuffle.cpp", "encode.hip", "worker.hip", "worker_f32_mfma.hip", "worker_bf16.hip", "fused_bf16.hip",
            "decode.hip", "onepass.hip", "transpose.hip", "runtime.hip", "shuffle.hip", "scratch.hip", "mx_quant.hip",
-           "mx_product.hip", "mx_few.hip", "mx_tiled.hip"]
+           "mx_product.hip", "mx_few.hip", "mx_tiled.hip", "mx_scaled.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result", f"-I{os.path.join(ROOT, 'include')}"]
 # Device code: gfx950 only; packed-fp32 instructions disabled.
@@ -40,7 +40,7 @@ def hipcc() -> str:
 # not overlap with the fp64 matrix work; the fp32 products at s = 16..64
 # measured 5% faster, the others unchanged).
 MFMA_VGPR_FORM = {"worker_f32_mfma.hip", "decode.hip", "worker_bf16.hip", "mx_few.hip",
-                  "mx_tiled.hip"}
+                  "mx_tiled.hip", "mx_scaled.hip"}
 
 
 def _compile(src: str, verbose: bool) -> str:

@@ -58,6 +58,10 @@ hipError_t launch_mx_few(const MxArgs& a, hipStream_t st);
 bool mx_tiled_serves(const MxArgs& a);
 int64_t mx_tiled_workspace_bytes(const MxArgs& a);
 hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st);
+// Both sides in 4 bits (mx_scaled.hip).
+bool mx_scaled_serves(const MxArgs& a);
+int64_t mx_scaled_workspace_bytes(const MxArgs& a);
+hipError_t launch_mx_scaled(const MxArgs& a, hipStream_t st);
 // Y from partial sums part[split][side][result] of n results a side, added in order.
 hipError_t launch_mx_join(const MxArgs& a, const float* part, int64_t splits, int64_t n, hipStream_t st);
 

@@ -124,11 +124,14 @@ hipError_t launch_bits(const MxArgs& a, hipStream_t st) {
 }  // namespace
 
 int64_t mx_workspace_bytes(const MxArgs& a) {
-    return mx_few_serves(a) ? mx_few_workspace_bytes(a) : mx_tiled_serves(a) ? mx_tiled_workspace_bytes(a) : 0;
+    if (mx_few_serves(a)) return mx_few_workspace_bytes(a);
+    if (mx_scaled_serves(a)) return mx_scaled_workspace_bytes(a);
+    return mx_tiled_serves(a) ? mx_tiled_workspace_bytes(a) : 0;
 }
 
 hipError_t launch_mx_product(const MxArgs& a, hipStream_t st) {
     if (mx_few_serves(a)) return launch_mx_few(a, st);
+    if (mx_scaled_serves(a)) return launch_mx_scaled(a, st);
     if (mx_tiled_serves(a)) return launch_mx_tiled(a, st);
     if (a.A.bits == 4) return a.trans ? launch_bits<4, true>(a, st) : launch_bits<4, false>(a, st);
     return a.trans ? launch_bits<8, true>(a, st) : launch_bits<8, false>(a, st);

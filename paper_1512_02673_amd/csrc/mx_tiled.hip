@@ -1,5 +1,5 @@
-// Products of a microscaled matrix with many dense right-hand sides, on the
-// bf16 matrix cores: out[i][j] = sum over k of P[i][k] Q[j][k], i a right-hand
+// Products of a microscaled matrix with many right-hand sides, on the bf16
+// matrix cores: out[i][j] = sum over k of P[i][k] Q[j][k], i a right-hand
 // side, j a result, Q the codes' values (exact in bf16).
 //
 // P is X in bf16 with k contiguous, rows of whole steps and 16-byte aligned: X
@@ -16,32 +16,12 @@
 // while the step before is computed, then into shared memory.
 #include <algorithm>
 
-#include "mx.h"
+#include "mx_tile.h"
 
 namespace coded {
 namespace {
 
-constexpr int kThreads = 256;
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
-typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef f32x4_t f32x4_any __attribute__((aligned(4)));
-typedef u32x2_t u32x2_any __attribute__((aligned(2)));
-
 constexpr int kStep = 64;   // terms
-
-// Loads within `bytes` of `base`; past them they give zeros.
-struct Window {
-    __amdgpu_buffer_rsrc_t rsrc;
-    __device__ __forceinline__ Window(const void* base, int64_t bytes)
-        : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, static_cast<int>(min<int64_t>(max<int64_t>(bytes, 0), 0xFFFFFFFF)),
-                                                 0x00027000)) {}
-    __device__ __forceinline__ u32x4_t four(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0); }
-    __device__ __forceinline__ uint32_t two_bytes(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0); }
-    __device__ __forceinline__ uint32_t byte(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b8(rsrc, at, 0, 0); }
-};
 
 struct TileArgs {
     const uint16_t* P;
@@ -55,55 +35,6 @@ struct TileArgs {
     int64_t tiles_i, tiles_j;
     int32_t flush;              // steps summed in one chain (fp32 results), 0: all
 };
-
-// A result's tile of four: results j .. j + 3 of side i (YROWS), or result j of sides i .. i + 3.
-template <bool YROWS>
-__device__ __forceinline__ void store_four(const MxArgs& a, float* part, int64_t n, int64_t i, int64_t j, f32x4_t v, bool first) {
-    const int64_t side = i, have = YROWS ? n - j : a.s - i;
-    if (have <= 0 || (YROWS ? i >= a.s : j >= n)) return;
-    if (part) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < have) part[YROWS ? side * n + j + e : (side + e) * n + j] = v[e];
-        return;
-    }
-    const int64_t at = YROWS ? i * a.ldy + j : j * a.ldy + i, ct = YROWS ? i * a.ldcc + j : j * a.ldcc + i;
-    v *= a.alpha;
-    if (a.C && first) {
-        float c[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (a.y_bf16)
-                c[e] = e < have ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(a.C)[ct + e]) << 16) : 0.f;
-            else
-                c[e] = e < have ? static_cast<const float*>(a.C)[ct + e] : 0.f;
-            v[e] = fmaf(a.beta, c[e], v[e]);
-        }
-    }
-    if (a.y_bf16) {
-        uint16_t* y = static_cast<uint16_t*>(a.Y) + at;
-        uint16_t b[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) b[e] = mx_to_bf16(v[e]);
-        if (have >= 4) {
-            *reinterpret_cast<u32x2_any*>(y) = u32x2_t{b[0] | static_cast<uint32_t>(b[1]) << 16, b[2] | static_cast<uint32_t>(b[3]) << 16};
-        } else {
-#pragma unroll
-            for (int e = 0; e < 3; ++e)
-                if (e < have) y[e] = b[e];
-        }
-    } else {
-        float* y = static_cast<float*>(a.Y) + at;
-        if (have >= 4) {
-            if (!first) v += *reinterpret_cast<const f32x4_any*>(y);
-            *reinterpret_cast<f32x4_any*>(y) = v;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 3; ++e)
-                if (e < have) y[e] = first ? v[e] : y[e] + v[e];
-        }
-    }
-}
 
 // Two waves along each side of the tile, each of TI x TJ tiles of 16 x 16.
 //
@@ -134,17 +65,8 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     const int64_t n = TRANS ? a.r : a.q;
     const int64_t blocks = ceil_div(a.r, kMxBlock), code_row = blocks * 4 * BITS;
 
-    // Workgroups go to the eight XCDs in turn: each takes a run of tiles of its own, in strips of 8 tiles of
-    // right-hand sides, so that what its L2 holds is used by several of them.
-    const int64_t total = g.tiles_i * g.tiles_j;
-    int64_t id = blockIdx.x % total;
-    const int64_t split = blockIdx.x / total;
-    {
-        const int64_t base = total / 8, rest = total % 8, x = id % 8, y = id / 8;
-        id = x * base + min(x, rest) + y;
-    }
-    const int64_t strip = id / (8 * g.tiles_j), in = id % (8 * g.tiles_j), high = min<int64_t>(8, g.tiles_i - strip * 8);
-    const int64_t i0 = (strip * 8 + in % high) * BI, j0 = in / high * BJ;
+    const TilePlace place = tile_place(g.tiles_i, g.tiles_j);
+    const int64_t split = place.split, i0 = place.i * BI, j0 = place.j * BJ;
 
     // what this thread loads of a step: byte offsets in the tile's rows
     const uint32_t p_at = static_cast<uint32_t>(tid / kPChunks * g.pitch * 2 + tid % kPChunks * 16);
@@ -308,6 +230,21 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     }
 }
 
+// A microscaled X in bf16 (exact), k contiguous: to[side][pitch], zeros from `terms` on.  A thread takes eight values.
+__global__ __launch_bounds__(256) void mx_unpack_kernel(MxMat x, int64_t s, int64_t terms, uint16_t* to, int64_t pitch) {
+    const int64_t id = blockIdx.x * int64_t(256) + threadIdx.x, per = pitch / 8;
+    const int64_t side = id / per, k = id % per * 8;
+    if (side >= s) return;
+    uint32_t v[4] = {0u, 0u, 0u, 0u};
+    if (k < terms) {   // up to the end of its last block a row's codes are zero
+        if (x.bits == 4)
+            mx_eight<4>(x.codes + side * x.ldc, x.scales + side * x.lds, k, v);
+        else
+            mx_eight<8>(x.codes + side * x.ldc, x.scales + side * x.lds, k, v);
+    }
+    *reinterpret_cast<u32x4_t*>(to + side * pitch + k) = u32x4_t{v[0], v[1], v[2], v[3]};
+}
+
 // X in bf16, k contiguous: to[plane][side][pitch], zeros from `terms` on.  A workgroup takes 64 sides x 64 terms.
 template <bool BF16>
 __global__ __launch_bounds__(256) void mx_pack_kernel(const void* X, int64_t ldx, int32_t x_rows, int64_t s, int64_t terms, uint16_t* to,
@@ -346,8 +283,7 @@ struct Plan {
     bool pack;          // X goes through the workspace
     int planes;
     int64_t steps, pitch, plane, pack_bytes;
-    bool large;         // tiles of 128 x 256, else 64 x 128
-    int64_t tiles_i, tiles_j, per, splits;
+    Cut cut;
     int64_t part_bytes;
 };
 
@@ -357,21 +293,14 @@ constexpr int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 Plan make_plan(const MxArgs& a, bool x) {
     Plan p{};
     const int64_t terms = a.trans ? a.q : a.r, n = a.trans ? a.r : a.q;
-    p.planes = a.x_bf16 ? 1 : 3;
+    p.planes = a.x_bits || a.x_bf16 ? 1 : 3;
     p.steps = ceil_div(terms, kStep);
     p.pitch = p.steps * kStep;
     p.plane = a.s * p.pitch;
-    p.pack = !(x && a.x_bf16 && a.x_rows && terms % kStep == 0 && a.ldx % 8 == 0 && (reinterpret_cast<uintptr_t>(a.X) & 15) == 0);
+    p.pack = !(x && !a.x_bits && a.x_bf16 && a.x_rows && terms % kStep == 0 && a.ldx % 8 == 0 && (reinterpret_cast<uintptr_t>(a.X) & 15) == 0);
     p.pack_bytes = round_up(p.planes * p.plane * 2, 256);
-    const int64_t wide = ceil_div(a.s, 128) * ceil_div(n, 256);
-    p.large = wide >= 256;
-    p.tiles_i = ceil_div(a.s, p.large ? 128 : 64);
-    p.tiles_j = ceil_div(n, p.large ? 256 : 128);
-    const int64_t steps = p.steps * p.planes;
-    p.splits = p.large ? 1 : std::max<int64_t>(1, std::min(512 / (p.tiles_i * p.tiles_j), steps / 4));
-    p.per = std::max<int64_t>(1, ceil_div(steps, p.splits));
-    p.splits = std::max<int64_t>(1, ceil_div(steps, p.per));
-    p.part_bytes = p.splits > 1 ? p.splits * a.s * n * 4 : 0;
+    p.cut = cut_tiles(a.s, n, p.steps * p.planes);
+    p.part_bytes = p.cut.splits > 1 ? p.cut.splits * a.s * n * 4 : 0;
     return p;
 }
 
@@ -390,7 +319,7 @@ hipError_t launch_tiles(const MxArgs& a, const TileArgs& g, bool large, hipStrea
 // Offsets within a tile's rows, of X and of codes, are 32-bit.
 bool mx_tiled_serves(const MxArgs& a) {
     const int64_t most = (int64_t(1) << 31) / 256;
-    return !a.x_bits && (a.trans ? a.q : a.r) < most / 2 && std::max(a.A.ldc, a.A.lds) < most && (!a.x_rows || a.ldx < most / 2);
+    return (a.trans ? a.q : a.r) < most / 2 && std::max(a.A.ldc, a.A.lds) < most && (!a.x_rows || a.ldx < most / 2);
 }
 
 int64_t mx_tiled_workspace_bytes(const MxArgs& a) {
@@ -408,14 +337,20 @@ hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
     g.row = p.pitch;
     g.planes = p.planes;
     g.steps = p.steps;
-    g.per = p.per;
-    g.splits = p.splits;
-    g.part = p.splits > 1 ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + p.pack_bytes) : nullptr;
-    g.tiles_i = p.tiles_i;
-    g.tiles_j = p.tiles_j;
+    g.per = p.cut.per;
+    g.splits = p.cut.splits;
+    g.part = p.cut.splits > 1 ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + p.pack_bytes) : nullptr;
+    g.tiles_i = p.cut.tiles_i;
+    g.tiles_j = p.cut.tiles_j;
     g.flush = a.y_bf16 || g.part ? 0 : 8192 / kStep;
-    if (!grid_fits(p.tiles_i * p.tiles_j * p.splits, kThreads)) return hipErrorInvalidConfiguration;
-    if (p.pack && p.pitch > 0) {
+    if (!grid_fits(p.cut.tiles_i * p.cut.tiles_j * p.cut.splits, kThreads)) return hipErrorInvalidConfiguration;
+    if (a.x_bits && p.pitch > 0) {
+        const int64_t blocks = ceil_div(a.s * (p.pitch / 8), 256);
+        if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+        mx_unpack_kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a.XM, a.s, terms, static_cast<uint16_t*>(a.workspace), p.pitch);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    } else if (p.pack && p.pitch > 0) {
         const int64_t blocks = ceil_div(p.pitch, 64) * ceil_div(a.s, 64);
         if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
         const auto kernel = a.x_bf16 ? mx_pack_kernel<true> : mx_pack_kernel<false>;
@@ -424,8 +359,8 @@ hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const hipError_t e = a.A.bits == 4 ? (a.trans ? launch_tiles<4, true>(a, g, p.large, st) : launch_tiles<4, false>(a, g, p.large, st))
-                                       : (a.trans ? launch_tiles<8, true>(a, g, p.large, st) : launch_tiles<8, false>(a, g, p.large, st));
+    const hipError_t e = a.A.bits == 4 ? (a.trans ? launch_tiles<4, true>(a, g, p.cut.large, st) : launch_tiles<4, false>(a, g, p.cut.large, st))
+                                       : (a.trans ? launch_tiles<8, true>(a, g, p.cut.large, st) : launch_tiles<8, false>(a, g, p.cut.large, st));
     if (e != hipSuccess || !g.part) return e;
     return launch_mx_join(a, g.part, g.splits, n, st);
 }

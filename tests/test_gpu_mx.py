@@ -87,7 +87,10 @@ def check_product(lib, torch, rng, transposed, q, r, s, bits, x, y, x_rows, y_ro
         cv = torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(dt).float().numpy().astype(np.float64)
         C = dense(torch, cv, dt, pad)
     A_ = A.T if transposed else A
-    want, size = A_ @ xv, np.abs(A_) @ np.abs(xv)
+    if whole:      # exact in 64 bits wherever it is computed
+        want = size = (torch.from_numpy(np.ascontiguousarray(A_)).cuda() @ torch.from_numpy(np.ascontiguousarray(xv)).cuda()).cpu().numpy()
+    else:
+        want, size = A_ @ xv, np.abs(A_) @ np.abs(xv)
     if y_rows:
         want, size = want.T, size.T
     want, size = alpha * want + beta * cv, abs(alpha) * size
@@ -225,6 +228,19 @@ def test_whole_numbers_are_exact(lib, torch, transposed, bits, x):
             if x.startswith("mx") and not order & 1:
                 continue
             check_product(lib, torch, rng, transposed, q, r, s, bits, x, "f32", bool(order & 1), bool(order & 2), whole=True)
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("x", ["f32", "bf16", "mx4", "mx8"])
+def test_whole_numbers_are_exact_in_large_tiles_and_long_sums(lib, torch, transposed, bits, x):
+    if transposed and x.startswith("mx"):
+        pytest.skip("U is dense")
+    rng = np.random.default_rng(13)
+    for n, k, s, order in [(8190, 130, 1030, 3), (8193, 8300, 1025, 1), (8193, 200, 1027, 0), (40, 20000, 100, 1), (300, 9000, 200, 3)]:
+        q, r = (k, n) if transposed else (n, k)
+        check_product(lib, torch, rng, transposed, q, r, s, bits, x, "f32", bool(order & 1) or x.startswith("mx"), bool(order & 2), whole=True,
+                      alpha=-1.0, beta=0.0)
 
 
 @pytest.mark.parametrize("transposed", [False, True])
