@@ -105,21 +105,50 @@ __device__ __forceinline__ bf16x8 operand(const u32x4_t* w, float scale) {
 
 // Y = A X.  A wave takes RT tiles of 16 rows.  Of every kStep terms lane (li,
 // lk) takes row li, blocks SB lk .. SB lk + SB - 1: 64 consecutive bytes of
-// codes and SB consecutive scale bytes; step (t, u) of the matrix instruction
-// takes values 8 u .. of its t-th block.  X lies in shared memory in that order,
-// so each operand is one 16-byte read, contiguous over the wave.  WK of the
-// eight waves share their rows and take every WK-th kStep; their sums are added
-// at the end.  Each kStep's sums start from zero and are added in fp32: a chain
-// of 512 terms, not of all of them.
+// codes and SB consecutive scale bytes; part (t, u) of the step takes values
+// 8 u .. of its t-th block.  X lies in shared memory in that order, so each
+// operand is one 16-byte read, contiguous over the wave.  WK of the eight waves
+// share their rows and take every WK-th step; their sums are added at the end.
+// Each step's sums start from zero and are added in fp32: a chain of 512 terms,
+// not of all of them.
+//
+// A short X is laid out in shared memory by every workgroup for itself, before
+// its loop.  Else mx_order_kernel has laid it out in the workspace, and the
+// workgroup copies what its waves' next steps need into the other half of
+// shared memory while they compute (ORDERED).
 //
 // Rows past q and blocks past r repeat the last one: such rows are not stored,
 // and such blocks meet zeros of X (a NaN in the last block is part of its row's
 // sums anyway).
-template <int BITS, int NT, int RT>
-__global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArgs a, int wk_log, int planes, int64_t kc) {
-    constexpr int SB = BITS == 4 ? 4 : 2;          // blocks a lane takes of a step
+template <int BITS>
+constexpr int kBlocksOf = BITS == 4 ? 4 : 2;            // blocks a lane takes of a step
+template <int BITS>
+constexpr int kStepOf = 128 * kBlocksOf<BITS>;          // terms
+
+// Where the eight terms from 8 g lie among pieces of eight, before the columns.
+template <int BITS>
+__device__ __forceinline__ int64_t ordered(int64_t g) {
+    constexpr int SB = kBlocksOf<BITS>;
+    const int b = static_cast<int>(g / 4 % (4 * SB)), u = static_cast<int>(g % 4);
+    return ((g / (16 * SB) * SB + b % SB) * 4 + u) * 4 + b / SB;
+}
+
+template <int BITS>
+__global__ __launch_bounds__(256) void mx_order_kernel(MxArgs a, int planes, int64_t pieces, u32x4_t* to) {
+    const int64_t id = blockIdx.x * int64_t(256) + threadIdx.x;
+    const int64_t g = a.x_rows ? id % pieces : id / a.s, c = a.x_rows ? id / pieces : id % a.s;
+    if (g >= pieces || c >= a.s) return;
+    u32x4_t v[3];
+    load_side(a, c, g * 8, a.r, v);
+    u32x4_t* at = to + ordered<BITS>(g) * planes * a.s + c;
+    for (int h = 0; h < planes; ++h) at[h * a.s] = h == 0 ? v[0] : h == 1 ? v[1] : v[2];
+}
+
+template <int BITS, int NT, int RT, bool ORDERED>
+__global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArgs a, int wk_log, int planes, const u32x4_t* image) {
+    constexpr int SB = kBlocksOf<BITS>, kStep = kStepOf<BITS>;
     constexpr int V = BITS == 4 ? 1 : 2;           // 16-byte loads of a block
-    constexpr int kStep = 128 * SB;
+    constexpr int kCopies = 8;                     // 16-byte pieces of X a thread copies for a step of each wave, at most
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -164,64 +193,89 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
     int col[NT];   // byte offset of this lane's column of a column tile
 #pragma unroll
     for (int n = 0; n < NT; ++n) col[n] = (16 * n + li < cols ? 16 * n + li : 0) * 16 + lk * cols * 16;
+    const int step_bytes = kStep * cols * 2;
 
     f32x4_t sum[RT][NT] = {};
-    int64_t mine = wk;   // this wave's next step
-    if (mine < steps) fetch(mine);
-    for (int64_t k0 = 0; k0 < a.r; k0 += kc) {
-        const int64_t end = min(k0 + kc, steps * kStep);
-        __syncthreads();
-        const int groups = static_cast<int>((end - k0) / 8);
-        for (int task = tid; task < groups * s; task += kThreads) {
-            const int g = a.x_rows ? task % groups : task / s, c = a.x_rows ? task / groups : task % s;
+    // a step's sums from X at xs; the next step's codes are on their way before they begin
+    const auto compute = [&](const char* xs, int64_t next) {
+        u32x4_t cw[RT][SB * V];
+        uint32_t cs[RT];
+#pragma unroll
+        for (int x = 0; x < RT; ++x) {
+            cs[x] = sc[x];
+#pragma unroll
+            for (int i = 0; i < SB * V; ++i) cw[x][i] = w[x][i];
+        }
+        if (next < steps) fetch(next);
+        f32x4_t acc[RT][NT] = {};
+#pragma unroll
+        for (int t = 0; t < SB; ++t) {
+            float scale[RT];
+#pragma unroll
+            for (int x = 0; x < RT; ++x) scale[x] = mx_scale((cs[x] >> (8 * t)) & 0xFFu);
+            const auto part = [&](auto U) {
+                bf16x8 xv[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    xv[n] = *reinterpret_cast<const bf16x8*>(xs + (t * 4 + U.value) * 4 * cols * 16 + col[n]);
+#pragma unroll
+                for (int x = 0; x < RT; ++x) {
+                    const bf16x8 av = operand<BITS, U.value>(&cw[x][t * V], scale[x]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        acc[x][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, xv[n], acc[x][n], 0, 0, 0);
+                }
+            };
+            part(std::integral_constant<int, 0>{});
+            part(std::integral_constant<int, 1>{});
+            part(std::integral_constant<int, 2>{});
+            part(std::integral_constant<int, 3>{});
+        }
+#pragma unroll
+        for (int x = 0; x < RT; ++x)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sum[x][n] += acc[x][n];
+    };
+
+    if (wk < steps) fetch(wk);
+    if constexpr (ORDERED) {
+        const int round = WK * step_bytes / 16;   // pieces of X of a round: one step of each of the WK waves
+        const int64_t pieces = steps * (step_bytes / 16);
+        u32x4_t xr[kCopies];
+        const auto copy_in = [&](int64_t first) {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                const int64_t at = first + tid + i * kThreads;
+                if (tid + i * kThreads < round && at < pieces) xr[i] = image[at];
+            }
+        };
+        const auto copy_out = [&](char* to) {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i)
+                if (tid + i * kThreads < round) *reinterpret_cast<u32x4_t*>(to + (tid + i * kThreads) * 16) = xr[i];
+        };
+        copy_in(0);
+        copy_out(smem);
+        int half = 0;
+        for (int64_t c = 0; c < steps; c += WK) {
+            __syncthreads();
+            const bool more = c + WK < steps;
+            if (more) copy_in((c + WK) * (step_bytes / 16));
+            if (c + wk < steps) compute(smem + half * round * 16 + wk * step_bytes, c + wk + WK);
+            half ^= 1;
+            if (more) copy_out(smem + half * round * 16);
+        }
+    } else {
+        const int pieces = static_cast<int>(steps) * (kStep / 8);
+        for (int task = tid; task < pieces * s; task += kThreads) {
+            const int g = a.x_rows ? task % pieces : task / s, c = a.x_rows ? task / pieces : task % s;
             u32x4_t v[3];
-            load_side(a, c, k0 + g * 8, a.r, v);
-            // group g: term 8 g of the chunk is in step (8 g) / kStep, block b of it, part u of the block
-            const int b = g / 4 % (4 * SB), u = g % 4, st = g / (16 * SB);
-            char* to = smem + (((st * SB + b % SB) * 4 + u) * 4 + b / SB) * cols * 16 + c * 16;
+            load_side(a, c, g * 8, a.r, v);
+            char* to = smem + (static_cast<int>(ordered<BITS>(g)) * cols + c) * 16;
             for (int h = 0; h < planes; ++h) *reinterpret_cast<u32x4_t*>(to + h * s * 16) = h == 0 ? v[0] : h == 1 ? v[1] : v[2];
         }
         __syncthreads();
-        for (; mine * kStep < end; mine += WK) {
-            u32x4_t cw[RT][SB * V];
-            uint32_t cs[RT];
-#pragma unroll
-            for (int x = 0; x < RT; ++x) {
-                cs[x] = sc[x];
-#pragma unroll
-                for (int i = 0; i < SB * V; ++i) cw[x][i] = w[x][i];
-            }
-            if (mine + WK < steps) fetch(mine + WK);
-            const char* xs = smem + static_cast<int>((mine * kStep - k0) / kStep) * (SB * 4 * 4) * cols * 16;
-            f32x4_t acc[RT][NT] = {};
-#pragma unroll
-            for (int t = 0; t < SB; ++t) {
-                float scale[RT];
-#pragma unroll
-                for (int x = 0; x < RT; ++x) scale[x] = mx_scale((cs[x] >> (8 * t)) & 0xFFu);
-                const auto part = [&](auto U) {
-                    bf16x8 xv[NT];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        xv[n] = *reinterpret_cast<const bf16x8*>(xs + (t * 4 + U.value) * 4 * cols * 16 + col[n]);
-#pragma unroll
-                    for (int x = 0; x < RT; ++x) {
-                        const bf16x8 av = operand<BITS, U.value>(&cw[x][t * V], scale[x]);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            acc[x][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, xv[n], acc[x][n], 0, 0, 0);
-                    }
-                };
-                part(std::integral_constant<int, 0>{});
-                part(std::integral_constant<int, 1>{});
-                part(std::integral_constant<int, 2>{});
-                part(std::integral_constant<int, 3>{});
-            }
-#pragma unroll
-            for (int x = 0; x < RT; ++x)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) sum[x][n] += acc[x][n];
-        }
+        for (int64_t m = wk; m < steps; m += WK) compute(smem + static_cast<int>(m) * step_bytes, m + WK);
     }
 
     // the waves' tiles through shared memory: rows x columns each, then the sums over waves and pieces
@@ -395,36 +449,59 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxArgs a, const float* par
 
 int planes_of(const MxArgs& a) { return a.x_bits || a.x_bf16 ? 1 : 3; }
 
-constexpr int64_t kXBytes = 64 << 10;   // of X in shared memory: two workgroups a compute unit
+// How a product along the blocks is cut up.
+struct FewPlan {
+    bool ordered;        // X goes through the workspace
+    int nt, rt, wk_log;  // column tiles, row tiles of a wave, log2 of the waves on the same rows
+    int64_t steps, lds, image_bytes;
+};
+FewPlan few_plan(const MxArgs& a) {
+    FewPlan p{};
+    const int64_t cols = planes_of(a) * a.s, step = a.A.bits == 4 ? 512 : 256;
+    p.nt = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
+    p.rt = p.nt == 1 ? 1 : 2;
+    p.steps = ceil_div(a.r, step);
+    const int64_t x_bytes = p.steps * step * cols * 2;
+    // Every workgroup lays out X for itself while that is at most two times eight values a thread, and 64 KB.
+    p.ordered = x_bytes > (64 << 10) || a.r * a.s > 16 * kThreads;
+    p.image_bytes = p.ordered ? x_bytes : 0;
+    // Waves on the same rows: until there are 2048 waves, as many as there are steps, and X's rounds for
+    // all of them fit twice into 64 KB (128 KB where a compute unit has one workgroup).
+    const int64_t tiles = ceil_div(a.q, 16 * p.rt), room = p.nt == 1 ? 64 << 10 : 128 << 10;
+    while (p.wk_log < 3 && (tiles << p.wk_log) < 2048 && (int64_t(2) << p.wk_log) <= p.steps &&
+           (!p.ordered || 2 * (step * cols * 2 << (p.wk_log + 1)) <= room))
+        ++p.wk_log;
+    const int64_t red = kWaves * 16 * p.rt * 16 * p.nt * 4;
+    p.lds = std::max(red, p.ordered ? 2 * (step * cols * 2 << p.wk_log) : x_bytes);
+    return p;
+}
 
 template <int BITS, int NT, int RT>
-hipError_t launch_few(const MxArgs& a, hipStream_t st) {
-    constexpr int64_t kStep = BITS == 4 ? 512 : 256;
+hipError_t launch_few(const MxArgs& a, const FewPlan& p, hipStream_t st) {
     const int planes = planes_of(a);
-    const int64_t cols = planes * a.s, steps = ceil_div(a.r, kStep);
-    // Waves on the same rows: as many as make 2048 of them, as X's share of shared memory holds a step for
-    // each, and as there are steps.
-    int wk_log = 0;
-    const int64_t tiles = ceil_div(a.q, 16 * RT);
-    while (wk_log < 3 && (tiles << wk_log) < 2048 && (int64_t(2) << wk_log) * kStep * cols * 2 <= kXBytes &&
-           (int64_t(2) << wk_log) <= steps)
-        ++wk_log;
-    const int64_t unit = kStep << wk_log;
-    const int64_t kc = std::max<int64_t>(1, std::min(kXBytes / (cols * 2) / unit, ceil_div(a.r, unit))) * unit;
-    const int64_t blocks = ceil_div(a.q, (kWaves >> wk_log) * 16 * RT);
+    const int64_t blocks = ceil_div(a.q, (kWaves >> p.wk_log) * 16 * RT);
     if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
-    const int64_t x_bytes = std::min(kc, steps * kStep) * cols * 2, red_bytes = kWaves * 16 * RT * 16 * NT * 4;
-    mx_few_kernel<BITS, NT, RT><<<dim3(static_cast<uint32_t>(blocks)), kThreads, std::max(x_bytes, red_bytes), st>>>(
-        a, wk_log, planes, kc);
+    const dim3 grid(static_cast<uint32_t>(blocks));
+    if (!p.ordered) {
+        mx_few_kernel<BITS, NT, RT, false><<<grid, kThreads, p.lds, st>>>(a, p.wk_log, planes, nullptr);
+        return hipGetLastError();
+    }
+    u32x4_t* image = static_cast<u32x4_t*>(a.workspace);
+    const int64_t pieces = p.steps * (kStepOf<BITS> / 8), groups = ceil_div(pieces * a.s, 256);
+    if (!grid_fits(groups, 256)) return hipErrorInvalidConfiguration;
+    mx_order_kernel<BITS><<<dim3(static_cast<uint32_t>(groups)), 256, 0, st>>>(a, planes, pieces, image);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    mx_few_kernel<BITS, NT, RT, true><<<grid, kThreads, p.lds, st>>>(a, p.wk_log, planes, image);
     return hipGetLastError();
 }
 
 template <int BITS>
 hipError_t launch_few_cols(const MxArgs& a, hipStream_t st) {
-    const int64_t cols = planes_of(a) * a.s;
-    if (cols <= 16) return launch_few<BITS, 1, 1>(a, st);
-    if (cols <= 32) return launch_few<BITS, 2, 2>(a, st);
-    return launch_few<BITS, 4, 2>(a, st);
+    const FewPlan p = few_plan(a);
+    if (p.nt == 1) return launch_few<BITS, 1, 1>(a, p, st);
+    if (p.nt == 2) return launch_few<BITS, 2, 2>(a, p, st);
+    return launch_few<BITS, 4, 2>(a, p, st);
 }
 
 // Workgroups that share the columns of mx_few_t_kernel: about 512 in all, each
@@ -469,7 +546,7 @@ bool mx_few_serves(const MxArgs& a) {
 }
 
 int64_t mx_few_workspace_bytes(const MxArgs& a) {
-    if (!a.trans) return 0;
+    if (!a.trans) return few_plan(a).image_bytes;
     const int64_t splits = ceil_div(a.q, t_rows(a));
     return splits > 1 ? splits * a.s * a.r * 4 : 0;
 }
