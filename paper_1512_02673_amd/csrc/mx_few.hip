@@ -85,52 +85,49 @@ __device__ __forceinline__ void load_side(const MxArgs& a, int64_t side, int64_t
     }
 }
 
-// Values 8 U .. 8 U + 7 of the 32 of a block as an operand of the matrix instruction.
+// Values 8 U .. 8 U + 7 of a 16-byte piece of codes (32 of 4 bits, 16 of 8) as an operand of the matrix instruction.
 template <int BITS, int U>
-__device__ __forceinline__ bf16x8 operand(const u32x4_t* w, float scale) {
+__device__ __forceinline__ bf16x8 operand(u32x4_t w, float scale) {
     u32x4_t v;
-    if constexpr (BITS == 4) {
-        const uint32_t c = w[0][U];
-        v = u32x4_t{mx_pair_bf16<4, 0>(c, scale), mx_pair_bf16<4, 1>(c, scale), mx_pair_bf16<4, 2>(c, scale),
-                    mx_pair_bf16<4, 3>(c, scale)};
-    } else {
-        const uint32_t c0 = w[U / 2][2 * (U & 1)], c1 = w[U / 2][2 * (U & 1) + 1];
-        v = u32x4_t{mx_pair_bf16<8, 0>(c0, scale), mx_pair_bf16<8, 1>(c0, scale), mx_pair_bf16<8, 0>(c1, scale),
-                    mx_pair_bf16<8, 1>(c1, scale)};
-    }
+    if constexpr (BITS == 4)
+        v = u32x4_t{mx_pair_bf16<4, 0>(w[U], scale), mx_pair_bf16<4, 1>(w[U], scale), mx_pair_bf16<4, 2>(w[U], scale),
+                    mx_pair_bf16<4, 3>(w[U], scale)};
+    else
+        v = u32x4_t{mx_pair_bf16<8, 0>(w[2 * U], scale), mx_pair_bf16<8, 1>(w[2 * U], scale), mx_pair_bf16<8, 0>(w[2 * U + 1], scale),
+                    mx_pair_bf16<8, 1>(w[2 * U + 1], scale)};
     return __builtin_bit_cast(bf16x8, v);
 }
 
 // ---------------------------------------------------------------- along the blocks
 
-// Y = A X.  A wave takes RT tiles of 16 rows.  Of every kStep terms lane (li,
-// lk) takes row li, blocks SB lk .. SB lk + SB - 1: 64 consecutive bytes of
-// codes and SB consecutive scale bytes; part (t, u) of the step takes values
-// 8 u .. of its t-th block.  X lies in shared memory in that order, so each
-// operand is one 16-byte read, contiguous over the wave.  WK of the eight waves
-// share their rows and take every WK-th step; their sums are added at the end.
-// Each step's sums start from zero and are added in fp32: a chain of 512 terms,
-// not of all of them.
+// Y = A X.  A wave takes RT tiles of 16 rows.  Of every step of 16 pieces (16
+// bytes: 32 or 16 codes) of a row lane (li, lk) takes row li, pieces 4 t + lk: a
+// load covers 64 consecutive bytes of each of 16 rows.  (Four consecutive pieces
+// a lane, which are the same bytes of a step, ran at 3.4 TB/s: each load then
+// touches every line of the step again.)  Part (t, u) takes values 8 u .. of the
+// t-th piece.  X lies in shared memory in that order, so each operand is one
+// 16-byte read, contiguous over the wave.  WK of the eight waves share their
+// rows and take every WK-th step; their sums are added at the end.  Each step's
+// sums start from zero and are added in fp32: a chain of 512 terms, not of all
+// of them.
 //
 // A short X is laid out in shared memory by every workgroup for itself, before
 // its loop.  Else mx_order_kernel has laid it out in the workspace, and the
 // workgroup copies what its waves' next steps need into the other half of
 // shared memory while they compute (ORDERED).
 //
-// Rows past q and blocks past r repeat the last one: such rows are not stored,
-// and such blocks meet zeros of X (a NaN in the last block is part of its row's
-// sums anyway).
+// Rows past q and pieces past a row's end repeat the last one: such rows are
+// not stored, and such pieces meet zeros of X (a NaN in the last block is part
+// of its row's sums anyway).
 template <int BITS>
-constexpr int kBlocksOf = BITS == 4 ? 4 : 2;            // blocks a lane takes of a step
-template <int BITS>
-constexpr int kStepOf = 128 * kBlocksOf<BITS>;          // terms
+constexpr int kStepOf = 16 * 128 / BITS;   // terms
 
 // Where the eight terms from 8 g lie among pieces of eight, before the columns.
 template <int BITS>
 __device__ __forceinline__ int64_t ordered(int64_t g) {
-    constexpr int SB = kBlocksOf<BITS>;
-    const int b = static_cast<int>(g / 4 % (4 * SB)), u = static_cast<int>(g % 4);
-    return ((g / (16 * SB) * SB + b % SB) * 4 + u) * 4 + b / SB;
+    constexpr int U = 16 / BITS;   // of a piece
+    const int64_t piece = g / U;
+    return (piece / 4 * U + g % U) * 4 + piece % 4;
 }
 
 template <int BITS>
@@ -146,8 +143,9 @@ __global__ __launch_bounds__(256) void mx_order_kernel(MxArgs a, int planes, int
 
 template <int BITS, int NT, int RT, bool ORDERED>
 __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArgs a, int wk_log, int planes, const u32x4_t* image) {
-    constexpr int SB = kBlocksOf<BITS>, kStep = kStepOf<BITS>;
-    constexpr int V = BITS == 4 ? 1 : 2;           // 16-byte loads of a block
+    constexpr int kStep = kStepOf<BITS>;
+    constexpr int U = 16 / BITS;                   // operands of a piece
+    constexpr int kScales = BITS == 4 ? 4 : 2;     // words of scales of a step
     constexpr int kCopies = 8;                     // 16-byte pieces of X a thread copies for a step of each wave, at most
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
@@ -164,27 +162,30 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
         codes[x] = a.A.codes + row * a.A.ldc;
         scales[x] = a.A.scales + row * a.A.lds;
     }
-    u32x4_t w[RT][SB * V];
-    uint32_t sc[RT];
+    u32x4_t w[RT][4];
+    uint32_t sc[RT][kScales];
+    const int64_t pieces_a = blocks * BITS / 4;
     const auto fetch = [&](int64_t step) {
+        const int64_t p0 = step * 16 + lk, b0 = step * kScales * 4;
+        if (step * 16 + 16 <= pieces_a) {
 #pragma unroll
-        for (int x = 0; x < RT; ++x) {
-            const int64_t b0 = step * 4 * SB + lk * SB;
-            if (b0 + SB <= blocks) {
-                const u32x4_t* p = reinterpret_cast<const u32x4_t*>(codes[x] + b0 * 16 * V);
+            for (int x = 0; x < RT; ++x) {
 #pragma unroll
-                for (int i = 0; i < SB * V; ++i) w[x][i] = __builtin_nontemporal_load(p + i);
-                sc[x] = SB == 4 ? *reinterpret_cast<const uint32_t*>(scales[x] + b0)
-                                : *reinterpret_cast<const uint16_t*>(scales[x] + b0);
-            } else {
-                sc[x] = 0;
+                for (int t = 0; t < 4; ++t) w[x][t] = *reinterpret_cast<const u32x4_t*>(codes[x] + (p0 + 4 * t) * 16);
 #pragma unroll
-                for (int t = 0; t < SB; ++t) {
-                    const int64_t b = min(b0 + t, blocks - 1);
-                    const u32x4_t* p = reinterpret_cast<const u32x4_t*>(codes[x] + b * 16 * V);
+                for (int i = 0; i < kScales; ++i) sc[x][i] = reinterpret_cast<const uint32_t*>(scales[x] + b0)[i];
+            }
+        } else {   // up to 16 pieces, the last step of a row
 #pragma unroll
-                    for (int i = 0; i < V; ++i) w[x][t * V + i] = p[i];
-                    sc[x] |= static_cast<uint32_t>(scales[x][b]) << (8 * t);
+            for (int x = 0; x < RT; ++x) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) w[x][t] = *reinterpret_cast<const u32x4_t*>(codes[x] + min(p0 + 4 * t, pieces_a - 1) * 16);
+#pragma unroll
+                for (int i = 0; i < kScales; ++i) {
+                    sc[x][i] = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        sc[x][i] |= static_cast<uint32_t>(scales[x][min(b0 + 4 * i + e, blocks - 1)]) << (8 * e);
                 }
             }
         }
@@ -198,29 +199,29 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
     f32x4_t sum[RT][NT] = {};
     // a step's sums from X at xs; the next step's codes are on their way before they begin
     const auto compute = [&](const char* xs, int64_t next) {
-        u32x4_t cw[RT][SB * V];
-        uint32_t cs[RT];
+        u32x4_t cw[RT][4];
+        float scale[RT][4];
 #pragma unroll
-        for (int x = 0; x < RT; ++x) {
-            cs[x] = sc[x];
+        for (int x = 0; x < RT; ++x)
 #pragma unroll
-            for (int i = 0; i < SB * V; ++i) cw[x][i] = w[x][i];
-        }
+            for (int t = 0; t < 4; ++t) {
+                cw[x][t] = w[x][t];
+                // piece 4 t + lk: byte lk of word t, or (two pieces a block) byte 2 t + lk / 2
+                const uint32_t byte = BITS == 4 ? sc[x][t] >> (8 * lk) : sc[x][t / 2] >> (16 * (t & 1) + 8 * (lk >> 1));
+                scale[x][t] = mx_scale(byte & 0xFFu);
+            }
         if (next < steps) fetch(next);
         f32x4_t acc[RT][NT] = {};
 #pragma unroll
-        for (int t = 0; t < SB; ++t) {
-            float scale[RT];
-#pragma unroll
-            for (int x = 0; x < RT; ++x) scale[x] = mx_scale((cs[x] >> (8 * t)) & 0xFFu);
-            const auto part = [&](auto U) {
+        for (int t = 0; t < 4; ++t) {
+            const auto part = [&](auto u) {
                 bf16x8 xv[NT];
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
-                    xv[n] = *reinterpret_cast<const bf16x8*>(xs + (t * 4 + U.value) * 4 * cols * 16 + col[n]);
+                    xv[n] = *reinterpret_cast<const bf16x8*>(xs + (t * U + u.value) * 4 * cols * 16 + col[n]);
 #pragma unroll
                 for (int x = 0; x < RT; ++x) {
-                    const bf16x8 av = operand<BITS, U.value>(&cw[x][t * V], scale[x]);
+                    const bf16x8 av = operand<BITS, u.value>(cw[x][t], scale[x][t]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
                         acc[x][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, xv[n], acc[x][n], 0, 0, 0);
@@ -228,8 +229,10 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
             };
             part(std::integral_constant<int, 0>{});
             part(std::integral_constant<int, 1>{});
-            part(std::integral_constant<int, 2>{});
-            part(std::integral_constant<int, 3>{});
+            if constexpr (U == 4) {
+                part(std::integral_constant<int, 2>{});
+                part(std::integral_constant<int, 3>{});
+            }
         }
 #pragma unroll
         for (int x = 0; x < RT; ++x)
@@ -326,7 +329,11 @@ __global__ __launch_bounds__(kThreads, 2) void mx_few_t_kernel(MxArgs a, int pla
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t group = blockIdx.x % groups, split = blockIdx.x / groups;
+    // Workgroups go to the eight XCDs in turn.  Those on the same rows share lines of scales (128 bytes
+    // are eight groups' scales of a row), so each XCD takes a run of them.
+    const int64_t base = gridDim.x / 8, rest = gridDim.x % 8, xcd = blockIdx.x % 8;
+    const int64_t id = xcd * base + min(xcd, rest) + blockIdx.x / 8;
+    const int64_t group = id % groups, split = id / groups;
     const int64_t t0 = split * per, t1 = min(t0 + per, a.q);
     const int s = static_cast<int>(a.s), cols = planes * s;
     const int64_t j0 = group * kCols;
