@@ -14,16 +14,13 @@
 // column's sums meet no other column's.
 #include <algorithm>
 
-#include "mx.h"
+#include "mx_window.h"
 
 namespace coded {
 namespace {
 
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 typedef u32x4_t u32x4_bf __attribute__((aligned(2)));
 typedef u32x4_t u32x4_f __attribute__((aligned(4)));
 
@@ -112,13 +109,15 @@ __device__ __forceinline__ bf16x8 operand(u32x4_t w, float scale) {
 // of them.
 //
 // A short X is laid out in shared memory by every workgroup for itself, before
-// its loop.  Else mx_order_kernel has laid it out in the workspace, and the
-// workgroup copies what its waves' next steps need into the other half of
-// shared memory while they compute (ORDERED).
+// its loop (COLS = 0).  Else mx_order_kernel has laid it out in the workspace, in
+// COLS columns, and the workgroup copies what its waves' next steps need, CP
+// pieces a thread, into the other half of shared memory while they compute.
 //
-// Rows past q and pieces past a row's end repeat the last one: such rows are
-// not stored, and such pieces meet zeros of X (a NaN in the last block is part
-// of its row's sums anyway).
+// All loads of the loop are issued in one straight line, a step ahead: rows past
+// q, pieces past a row's end and steps past the last are addressed past the end
+// of a bounded buffer, which reads as zeros and moves nothing, and the scale
+// bytes past the last block are cleared.  (With branches around the loads the
+// compiler waits for all that are in flight at each of them.)
 template <int BITS>
 constexpr int kStepOf = 16 * 128 / BITS;   // terms
 
@@ -131,76 +130,81 @@ __device__ __forceinline__ int64_t ordered(int64_t g) {
 }
 
 template <int BITS>
-__global__ __launch_bounds__(256) void mx_order_kernel(MxArgs a, int planes, int64_t pieces, u32x4_t* to) {
+__global__ __launch_bounds__(256) void mx_order_kernel(MxArgs a, int planes, int64_t pieces, int cols, u32x4_t* to) {
     const int64_t id = blockIdx.x * int64_t(256) + threadIdx.x;
     const int64_t g = a.x_rows ? id % pieces : id / a.s, c = a.x_rows ? id / pieces : id % a.s;
     if (g >= pieces || c >= a.s) return;
     u32x4_t v[3];
     load_side(a, c, g * 8, a.r, v);
-    u32x4_t* at = to + ordered<BITS>(g) * planes * a.s + c;
+    u32x4_t* at = to + ordered<BITS>(g) * cols + c;
     for (int h = 0; h < planes; ++h) at[h * a.s] = h == 0 ? v[0] : h == 1 ? v[1] : v[2];
 }
 
-template <int BITS, int NT, int RT, bool ORDERED>
-__global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArgs a, int wk_log, int planes, const u32x4_t* image) {
+template <int BITS, int NT, int RT, int COLS, int CP>
+__global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArgs a, int wk_log_, int planes, const u32x4_t* image) {
     constexpr int kStep = kStepOf<BITS>;
     constexpr int U = 16 / BITS;                   // operands of a piece
     constexpr int kScales = BITS == 4 ? 4 : 2;     // words of scales of a step
-    constexpr int kCopies = 8;                     // 16-byte pieces of X a thread copies for a step of each wave, at most
+    constexpr uint32_t kNowhere = 0xFFFFFFF0u;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int WK = 1 << wk_log, wk = wave & (WK - 1), wr = wave >> wk_log;
-    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * (kWaves >> wk_log) * 16 * RT;
-    const int s = static_cast<int>(a.s), cols = planes * s;
-    const int64_t blocks = ceil_div(a.r, kMxBlock), steps = ceil_div(a.r, kStep);
+    // waves on the same rows: with COLS, as many as share the pieces of X that are copied at once
+    const int WK = COLS ? CP * kThreads / (kStep / 8 * (COLS ? COLS : 1)) : 1 << wk_log_;
+    const int wk = wave & (WK - 1), wr = wave / WK;
+    const int s = static_cast<int>(a.s), cols = planes * s, pitch = COLS ? COLS : cols;   // pitch: columns that X is laid out in
+    const int rows = kWaves / WK * 16 * RT;
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * rows;
+    const int64_t blocks = ceil_div(a.r, kMxBlock), pieces_a = blocks * BITS / 4, steps = ceil_div(a.r, kStep);
 
-    const uint8_t *codes[RT], *scales[RT];
+    const int64_t have = lesser(a.q - row0, rows) - 1;
+    const Window codes(a.A.codes + row0 * a.A.ldc, have * a.A.ldc + pieces_a * 16);
+    const Window scales(a.A.scales + row0 * a.A.lds, have * a.A.lds + ceil_div(blocks, 4) * 4);
+    uint32_t code_row[RT], scale_row[RT];
 #pragma unroll
     for (int x = 0; x < RT; ++x) {
-        const int64_t row = min(row0 + (wr * RT + x) * 16 + li, a.q - 1);
-        codes[x] = a.A.codes + row * a.A.ldc;
-        scales[x] = a.A.scales + row * a.A.lds;
+        const uint32_t row = (wr * RT + x) * 16 + li;
+        code_row[x] = row * static_cast<uint32_t>(a.A.ldc);
+        scale_row[x] = row * static_cast<uint32_t>(a.A.lds);
     }
     u32x4_t w[RT][4];
-    uint32_t sc[RT][kScales];
-    const int64_t pieces_a = blocks * BITS / 4;
-    const auto fetch = [&](int64_t step) {
-        const int64_t p0 = step * 16 + lk, b0 = step * kScales * 4;
-        if (step * 16 + 16 <= pieces_a) {
+    typedef unsigned int scales_t __attribute__((ext_vector_type(kScales)));
+    scales_t sc[RT];
+    const auto fetch = [&](int step) {
+        const int p0 = step * 16 + lk, b0 = step * kScales * 4;
 #pragma unroll
-            for (int x = 0; x < RT; ++x) {
+        for (int t = 0; t < 4; ++t) {
+            const bool in = p0 + 4 * t < static_cast<int>(pieces_a);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) w[x][t] = *reinterpret_cast<const u32x4_t*>(codes[x] + (p0 + 4 * t) * 16);
+            for (int x = 0; x < RT; ++x) w[x][t] = codes.four(in ? code_row[x] + (p0 + 4 * t) * 16 : kNowhere);
+        }
 #pragma unroll
-                for (int i = 0; i < kScales; ++i) sc[x][i] = reinterpret_cast<const uint32_t*>(scales[x] + b0)[i];
-            }
-        } else {   // up to 16 pieces, the last step of a row
-#pragma unroll
-            for (int x = 0; x < RT; ++x) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t) w[x][t] = *reinterpret_cast<const u32x4_t*>(codes[x] + min(p0 + 4 * t, pieces_a - 1) * 16);
-#pragma unroll
-                for (int i = 0; i < kScales; ++i) {
-                    sc[x][i] = 0;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        sc[x][i] |= static_cast<uint32_t>(scales[x][min(b0 + 4 * i + e, blocks - 1)]) << (8 * e);
-                }
-            }
+        for (int x = 0; x < RT; ++x) {
+            const uint32_t at = p0 < static_cast<int>(pieces_a) + lk ? scale_row[x] + b0 : kNowhere;   // the step's first piece is in the row
+            if constexpr (BITS == 4)
+                sc[x] = scales.four(at);
+            else
+                sc[x] = scales.two(at);
         }
     };
 
     int col[NT];   // byte offset of this lane's column of a column tile
 #pragma unroll
-    for (int n = 0; n < NT; ++n) col[n] = (16 * n + li < cols ? 16 * n + li : 0) * 16 + lk * cols * 16;
-    const int step_bytes = kStep * cols * 2;
+    for (int n = 0; n < NT; ++n) col[n] = (16 * n + li < pitch ? 16 * n + li : 0) * 16 + lk * pitch * 16;
+    const int step_bytes = kStep * pitch * 2;
 
     f32x4_t sum[RT][NT] = {};
     // a step's sums from X at xs; the next step's codes are on their way before they begin
-    const auto compute = [&](const char* xs, int64_t next) {
+    const auto compute = [&](const char* xs, int step, int next) {
         u32x4_t cw[RT][4];
         float scale[RT][4];
+        const int left = static_cast<int>(blocks) - step * kScales * 4;
+        if (left < 4 * kScales) {   // the row's last step
+#pragma unroll
+            for (int i = 0; i < kScales; ++i)
+#pragma unroll
+                for (int x = 0; x < RT; ++x) sc[x][i] &= left >= 4 * i + 4 ? ~0u : left <= 4 * i ? 0u : (1u << (8 * (left - 4 * i))) - 1;
+        }
 #pragma unroll
         for (int x = 0; x < RT; ++x)
 #pragma unroll
@@ -210,75 +214,82 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
                 const uint32_t byte = BITS == 4 ? sc[x][t] >> (8 * lk) : sc[x][t / 2] >> (16 * (t & 1) + 8 * (lk >> 1));
                 scale[x][t] = mx_scale(byte & 0xFFu);
             }
-        if (next < steps) fetch(next);
+        fetch(next);
         f32x4_t acc[RT][NT] = {};
+        // X's operands are read one part ahead
+        bf16x8 xv[2][NT];
+        const auto read = [&](int p) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const auto part = [&](auto u) {
-                bf16x8 xv[NT];
+            for (int n = 0; n < NT; ++n) xv[p & 1][n] = *reinterpret_cast<const bf16x8*>(xs + p * 4 * pitch * 16 + col[n]);
+        };
+        const auto part = [&](auto P) {
+            constexpr int p = P.value;
+            if constexpr (p + 1 < 4 * U) read(p + 1);
+#pragma unroll
+            for (int x = 0; x < RT; ++x) {
+                const bf16x8 av = operand<BITS, p % U>(cw[x][p / U], scale[x][p / U]);
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
-                    xv[n] = *reinterpret_cast<const bf16x8*>(xs + (t * U + u.value) * 4 * cols * 16 + col[n]);
-#pragma unroll
-                for (int x = 0; x < RT; ++x) {
-                    const bf16x8 av = operand<BITS, u.value>(cw[x][t], scale[x][t]);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        acc[x][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, xv[n], acc[x][n], 0, 0, 0);
-                }
-            };
-            part(std::integral_constant<int, 0>{});
-            part(std::integral_constant<int, 1>{});
-            if constexpr (U == 4) {
-                part(std::integral_constant<int, 2>{});
-                part(std::integral_constant<int, 3>{});
+                    acc[x][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, xv[p & 1][n], acc[x][n], 0, 0, 0);
             }
-        }
+            if constexpr (NT > 1) __builtin_amdgcn_sched_barrier(0);
+        };
+        read(0);
+        [&]<int... P>(std::integer_sequence<int, P...>) { (part(std::integral_constant<int, P>{}), ...); }(std::make_integer_sequence<int, 4 * U>{});
 #pragma unroll
         for (int x = 0; x < RT; ++x)
 #pragma unroll
             for (int n = 0; n < NT; ++n) sum[x][n] += acc[x][n];
     };
 
-    if (wk < steps) fetch(wk);
-    if constexpr (ORDERED) {
-        const int round = WK * step_bytes / 16;   // pieces of X of a round: one step of each of the WK waves
-        const int64_t pieces = steps * (step_bytes / 16);
-        u32x4_t xr[kCopies];
-        const auto copy_in = [&](int64_t first) {
+    // Rounds of one step of each of the WK waves.  Workgroups start at different ones: in step, they would all
+    // read the same columns of their rows, a whole row apart.
+    const int rounds = static_cast<int>(ceil_div(steps, WK)), none = static_cast<int>(steps) + WK;
+    int c = blockIdx.x % rounds;
+    fetch(c * WK + wk);
+    if constexpr (COLS) {
+        const int round = WK * step_bytes;
+        const Window x(image, steps * step_bytes);
+        u32x4_t xr[CP];
+        const auto copy_in = [&](int64_t r) {
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i) {
-                const int64_t at = first + tid + i * kThreads;
-                if (tid + i * kThreads < round && at < pieces) xr[i] = image[at];
-            }
+            for (int i = 0; i < CP; ++i) xr[i] = x.four(static_cast<uint32_t>(r * round) + (tid + i * kThreads) * 16);
         };
         const auto copy_out = [&](char* to) {
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i)
-                if (tid + i * kThreads < round) *reinterpret_cast<u32x4_t*>(to + (tid + i * kThreads) * 16) = xr[i];
+            for (int i = 0; i < CP; ++i) *reinterpret_cast<u32x4_t*>(to + (tid + i * kThreads) * 16) = xr[i];
         };
-        copy_in(0);
+        copy_in(c);
         copy_out(smem);
         int half = 0;
-        for (int64_t c = 0; c < steps; c += WK) {
+        for (int i = 0; i < rounds; ++i) {
             __syncthreads();
-            const bool more = c + WK < steps;
-            if (more) copy_in((c + WK) * (step_bytes / 16));
-            if (c + wk < steps) compute(smem + half * round * 16 + wk * step_bytes, c + wk + WK);
+            const int next = c + 1 < rounds ? c + 1 : 0;
+            copy_in(next);
+            compute(smem + half * round + wk * step_bytes, c * WK + wk, i + 1 < rounds ? next * WK + wk : none);
+            c = next;
             half ^= 1;
-            if (more) copy_out(smem + half * round * 16);
+            copy_out(smem + half * round);
         }
     } else {
         const int pieces = static_cast<int>(steps) * (kStep / 8);
         for (int task = tid; task < pieces * s; task += kThreads) {
-            const int g = a.x_rows ? task % pieces : task / s, c = a.x_rows ? task / pieces : task % s;
+            const int g = a.x_rows ? task % pieces : task / s, side = a.x_rows ? task / pieces : task % s;
             u32x4_t v[3];
-            load_side(a, c, g * 8, a.r, v);
-            char* to = smem + (static_cast<int>(ordered<BITS>(g)) * cols + c) * 16;
+            load_side(a, side, g * 8, a.r, v);
+            char* to = smem + (static_cast<int>(ordered<BITS>(g)) * cols + side) * 16;
             for (int h = 0; h < planes; ++h) *reinterpret_cast<u32x4_t*>(to + h * s * 16) = h == 0 ? v[0] : h == 1 ? v[1] : v[2];
         }
         __syncthreads();
-        for (int64_t m = wk; m < steps; m += WK) compute(smem + static_cast<int>(m) * step_bytes, m + WK);
+        for (int i = 0; i < rounds; ++i) {
+            const int next = c + 1 < rounds ? c + 1 : 0, m = c * WK + wk;
+            const int then = i + 1 < rounds ? next * WK + wk : none;
+            if (m < steps)
+                compute(smem + m * step_bytes, m, then);
+            else
+                fetch(then);
+            c = next;
+        }
     }
 
     // the waves' tiles through shared memory: rows x columns each, then the sums over waves and pieces
@@ -291,9 +302,8 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int v = 0; v < 4; ++v)
-                red[((wk * (kWaves >> wk_log) + wr) * RT * 16 + x * 16 + 4 * lk + v) * kPitch + 16 * n + li] = sum[x][n][v];
+                red[(wk * rows + (wr * RT + x) * 16 + 4 * lk + v) * kPitch + 16 * n + li] = sum[x][n][v];
     __syncthreads();
-    const int rows = (kWaves >> wk_log) * RT * 16;
     for (int task = tid; task < rows * s; task += kThreads) {
         const int t = a.y_rows ? task % rows : task / s, c = a.y_rows ? task / rows : task % s;
         if (row0 + t >= a.q) continue;
@@ -332,32 +342,34 @@ __global__ __launch_bounds__(kThreads, 2) void mx_few_t_kernel(MxArgs a, int pla
     // Workgroups go to the eight XCDs in turn.  Those on the same rows share lines of scales (128 bytes
     // are eight groups' scales of a row), so each XCD takes a run of them.
     const int64_t base = gridDim.x / 8, rest = gridDim.x % 8, xcd = blockIdx.x % 8;
-    const int64_t id = xcd * base + min(xcd, rest) + blockIdx.x / 8;
+    const int64_t id = xcd * base + lesser(xcd, rest) + blockIdx.x / 8;
     const int64_t group = id % groups, split = id / groups;
-    const int64_t t0 = split * per, t1 = min(t0 + per, a.q);
+    const int64_t t0 = split * per, t1 = lesser(t0 + per, a.q);
     const int s = static_cast<int>(a.s), cols = planes * s;
     const int64_t j0 = group * kCols;
-    // this lane's columns, moved back to the last whole piece
-    const int64_t j = min(j0 + li * CW, ceil_div(a.r, kMxBlock) * kMxBlock - CW);
-    const uint8_t* codes = a.A.codes + j * BITS / 8;
-    const uint8_t* scales = a.A.scales + j / kMxBlock;
     typedef unsigned int words_t __attribute__((ext_vector_type(W / 4)));
+    static_assert(W == 16, "");
     words_t w[8];
     uint32_t sc[8];
+    // rows past q read as zeros; columns past r are other bytes of A, or zeros, and are not stored
+    const int64_t blocks = ceil_div(a.r, kMxBlock), c0_ = j0 * BITS / 8, b0_ = j0 / kMxBlock;
+    const uint32_t code_at = static_cast<uint32_t>(8 * lk * a.A.ldc) + li * W, scale_at = static_cast<uint32_t>(8 * lk * a.A.lds) + li * CW / kMxBlock;
     const auto fetch = [&](int64_t t) {
+        const int64_t have = lesser(a.q - t, 32) - 1;
+        const Window codes(a.A.codes + t * a.A.ldc + c0_, have < 0 ? 0 : have * a.A.ldc + blocks * 4 * BITS - c0_);
+        const Window scales(a.A.scales + t * a.A.lds + b0_, have < 0 ? 0 : have * a.A.lds + blocks - b0_);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int64_t row = min(t + 8 * lk + e, a.q - 1);
-            w[e] = __builtin_nontemporal_load(reinterpret_cast<const words_t*>(codes + row * a.A.ldc));
-            sc[e] = scales[row * a.A.lds];
+            w[e] = codes.four(code_at + static_cast<uint32_t>(e * a.A.ldc));
+            sc[e] = scales.byte(scale_at + static_cast<uint32_t>(e * a.A.lds));
         }
     };
     f32x4_t acc[CW] = {};
     const int col = (li < cols ? li : 0) * 16 + lk * cols * 16;
     int64_t mine = t0 + wave * 32;
-    if (mine < t1) fetch(mine);
+    fetch(lesser(mine, a.q));
     for (int64_t c0 = t0; c0 < t1; c0 += rows_staged) {
-        const int64_t end = min(c0 + rows_staged, t1);
+        const int64_t end = lesser(c0 + rows_staged, t1);
         __syncthreads();
         const int pieces = static_cast<int>(ceil_div(end - c0, 32)) * 4;
         for (int task = tid; task < pieces * s; task += kThreads) {
@@ -377,7 +389,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_few_t_kernel(MxArgs a, int pla
                 cw[e] = w[e];
                 scale[e] = mx_scale(sc[e]);
             }
-            if (mine + 32 * kWaves < t1) fetch(mine + 32 * kWaves);
+            fetch(mine + 32 * kWaves < t1 ? mine + 32 * kWaves : a.q);
             // a word holds 8 (4) columns: pairs of them, then down the rows
             const auto pair = [&](auto P, int word) {
                 uint32_t v[8];
@@ -458,57 +470,74 @@ int planes_of(const MxArgs& a) { return a.x_bits || a.x_bf16 ? 1 : 3; }
 
 // How a product along the blocks is cut up.
 struct FewPlan {
-    bool ordered;        // X goes through the workspace
-    int nt, rt, wk_log;  // column tiles, row tiles of a wave, log2 of the waves on the same rows
+    int cols;            // that X is laid out in in the workspace; 0: it is not
+    int rt, wk_log;      // row tiles of a wave, log2 of the waves on the same rows
     int64_t steps, lds, image_bytes;
 };
 FewPlan few_plan(const MxArgs& a) {
     FewPlan p{};
     const int64_t cols = planes_of(a) * a.s, step = a.A.bits == 4 ? 512 : 256;
-    p.nt = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
-    p.rt = p.nt == 1 ? 1 : 2;
     p.steps = ceil_div(a.r, step);
     const int64_t x_bytes = p.steps * step * cols * 2;
     // Every workgroup lays out X for itself while that is at most two times eight values a thread, and 64 KB.
-    p.ordered = x_bytes > (64 << 10) || a.r * a.s > 16 * kThreads;
-    p.image_bytes = p.ordered ? x_bytes : 0;
-    // Waves on the same rows: until there are 2048 waves, as many as there are steps, and X's rounds for
-    // all of them fit twice into 64 KB (128 KB where a compute unit has one workgroup).
-    const int64_t tiles = ceil_div(a.q, 16 * p.rt), room = p.nt == 1 ? 64 << 10 : 128 << 10;
+    const bool ordered = cols > 16 || x_bytes > (64 << 10) || a.r * a.s > 16 * kThreads;
+    p.cols = !ordered ? 0 : cols <= 8 ? 8 : cols <= 16 ? 16 : cols <= 32 ? 32 : 64;
+    p.rt = cols <= 16 ? 1 : 2;
+    p.image_bytes = p.steps * step * p.cols * 2;
+    // Waves on the same rows: until there are 2048 waves, as many as there are steps.  X's pieces of a round,
+    // twice, take up to 64 KB (128 KB where the registers leave a compute unit one workgroup anyway), and
+    // at least one piece is each thread's.
+    const int64_t tiles = ceil_div(a.q, 16 * p.rt), room = p.rt == 1 ? 64 << 10 : 128 << 10;
+    if (p.cols && step / 8 * p.cols < kThreads) p.wk_log = 1;
     while (p.wk_log < 3 && (tiles << p.wk_log) < 2048 && (int64_t(2) << p.wk_log) <= p.steps &&
-           (!p.ordered || 2 * (step * cols * 2 << (p.wk_log + 1)) <= room))
+           2 * (step * p.cols * 2 << (p.wk_log + 1)) <= room)
         ++p.wk_log;
-    const int64_t red = kWaves * 16 * p.rt * 16 * p.nt * 4;
-    p.lds = std::max(red, p.ordered ? 2 * (step * cols * 2 << p.wk_log) : x_bytes);
+    const int64_t red = kWaves * 16 * p.rt * 16 * (cols <= 16 ? 1 : p.cols / 16) * 4;
+    p.lds = std::max(red, p.cols ? 2 * (step * p.cols * 2 << p.wk_log) : x_bytes);
     return p;
 }
 
-template <int BITS, int NT, int RT>
+template <int BITS, int NT, int RT, int COLS, int CP>
 hipError_t launch_few(const MxArgs& a, const FewPlan& p, hipStream_t st) {
+    if constexpr (CP * kThreads < kStepOf<BITS> / 8 * COLS) {   // less than a step of X a round
+        return hipErrorInvalidConfiguration;
+    } else {
     const int planes = planes_of(a);
     const int64_t blocks = ceil_div(a.q, (kWaves >> p.wk_log) * 16 * RT);
     if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
-    const dim3 grid(static_cast<uint32_t>(blocks));
-    if (!p.ordered) {
-        mx_few_kernel<BITS, NT, RT, false><<<grid, kThreads, p.lds, st>>>(a, p.wk_log, planes, nullptr);
-        return hipGetLastError();
-    }
     u32x4_t* image = static_cast<u32x4_t*>(a.workspace);
-    const int64_t pieces = p.steps * (kStepOf<BITS> / 8), groups = ceil_div(pieces * a.s, 256);
-    if (!grid_fits(groups, 256)) return hipErrorInvalidConfiguration;
-    mx_order_kernel<BITS><<<dim3(static_cast<uint32_t>(groups)), 256, 0, st>>>(a, planes, pieces, image);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    mx_few_kernel<BITS, NT, RT, true><<<grid, kThreads, p.lds, st>>>(a, p.wk_log, planes, image);
+    if constexpr (COLS) {
+        const int64_t pieces = p.steps * (kStepOf<BITS> / 8), groups = ceil_div(pieces * a.s, 256);
+        if (!grid_fits(groups, 256)) return hipErrorInvalidConfiguration;
+        mx_order_kernel<BITS><<<dim3(static_cast<uint32_t>(groups)), 256, 0, st>>>(a, planes, pieces, COLS, image);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    mx_few_kernel<BITS, NT, RT, COLS, CP><<<dim3(static_cast<uint32_t>(blocks)), kThreads, p.lds, st>>>(a, p.wk_log, planes, image);
     return hipGetLastError();
+    }
 }
 
 template <int BITS>
 hipError_t launch_few_cols(const MxArgs& a, hipStream_t st) {
     const FewPlan p = few_plan(a);
-    if (p.nt == 1) return launch_few<BITS, 1, 1>(a, p, st);
-    if (p.nt == 2) return launch_few<BITS, 2, 2>(a, p, st);
-    return launch_few<BITS, 4, 2>(a, p, st);
+    // pieces of X a thread copies a round
+    const int cp = static_cast<int>((kStepOf<BITS> / 8 * p.cols << p.wk_log) / kThreads);
+    switch (p.cols * 16 + cp) {
+        case 0: return launch_few<BITS, 1, 1, 0, 1>(a, p, st);
+        case 8 * 16 + 1: return launch_few<BITS, 1, 1, 8, 1>(a, p, st);
+        case 8 * 16 + 2: return launch_few<BITS, 1, 1, 8, 2>(a, p, st);
+        case 8 * 16 + 4: return launch_few<BITS, 1, 1, 8, 4>(a, p, st);
+        case 16 * 16 + 1: return launch_few<BITS, 1, 1, 16, 1>(a, p, st);
+        case 16 * 16 + 2: return launch_few<BITS, 1, 1, 16, 2>(a, p, st);
+        case 16 * 16 + 4: return launch_few<BITS, 1, 1, 16, 4>(a, p, st);
+        case 32 * 16 + 2: return launch_few<BITS, 2, 2, 32, 2>(a, p, st);
+        case 32 * 16 + 4: return launch_few<BITS, 2, 2, 32, 4>(a, p, st);
+        case 32 * 16 + 8: return launch_few<BITS, 2, 2, 32, 8>(a, p, st);
+        case 64 * 16 + 4: return launch_few<BITS, 4, 2, 64, 4>(a, p, st);
+        case 64 * 16 + 8: return launch_few<BITS, 4, 2, 64, 8>(a, p, st);
+        default: return hipErrorInvalidConfiguration;
+    }
 }
 
 // Workgroups that share the columns of mx_few_t_kernel: about 512 in all, each
@@ -549,7 +578,9 @@ hipError_t launch_mx_join(const MxArgs& a, const float* part, int64_t splits, in
 
 bool mx_few_serves(const MxArgs& a) {
     const int64_t terms = a.trans ? a.q : a.r;
-    return terms > 0 && a.s <= 64 && planes_of(a) * a.s <= (a.trans ? 16 : 64);
+    // offsets within a workgroup's rows, and steps, are 32-bit
+    const int64_t most = (int64_t(1) << 31) / 256;
+    return terms > 0 && a.s <= 64 && planes_of(a) * a.s <= (a.trans ? 16 : 64) && std::max(a.A.ldc, a.A.lds) < most;
 }
 
 int64_t mx_few_workspace_bytes(const MxArgs& a) {

@@ -45,7 +45,7 @@ struct Panel {
 #pragma unroll
         for (int l = 0; l < kLoads; ++l)
             next[l] = codes.four(static_cast<uint32_t>((tid / kPieces + l * (kThreads / kPieces)) * m.ldc + tid % kPieces * 16));
-        scale = scales.word(static_cast<uint32_t>(min(tid, ROWS - 1) * m.lds));
+        scale = scales.word(static_cast<uint32_t>(lesser(tid, ROWS - 1) * m.lds));
         if (b0 + 4 > blocks) {
             const int have = static_cast<int>(blocks - b0);
             scale &= (1u << (8 * have)) - 1;
@@ -55,7 +55,7 @@ struct Panel {
         }
     }
     static __device__ __forceinline__ int place(int row, int piece) {
-        return row * kRow + ((piece + (row >> 2)) & 3) * 16;   // the 16 rows of an operand on all banks
+        return row * kRow + (piece ^ row_group(row)) * 16;
     }
     __device__ __forceinline__ void stage(char* codes, uint32_t* scales) const {
         const int tid = threadIdx.x;
@@ -137,13 +137,13 @@ __global__ __launch_bounds__(kThreads, 2) void mx_scaled_kernel(MxArgs a, Scaled
     };
 
     int64_t t = place.split * g.per;
-    const int64_t t1 = min(t + g.per, g.steps);
+    const int64_t t1 = lesser(t + g.per, g.steps);
     if (t < t1) {
         fetch(t);
         stage();
     }
     for (bool first = true;; first = false) {
-        const int64_t end = g.flush ? min(t + g.flush, t1) : t1;
+        const int64_t end = g.flush ? lesser(t + g.flush, t1) : t1;
         for (; t < end; ++t) {
             __syncthreads();
             if (t + 1 < t1) fetch(t + 1);

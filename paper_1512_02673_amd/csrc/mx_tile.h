@@ -4,33 +4,12 @@
 
 #include <algorithm>
 
-#include "mx.h"
+#include "mx_window.h"
 
 namespace coded {
 namespace {
 
 constexpr int kThreads = 256;   // of a tile's workgroup: two waves along each of its sides
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
-typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef f32x4_t f32x4_any __attribute__((aligned(4)));
-typedef u32x2_t u32x2_any __attribute__((aligned(2)));
-
-
-// Loads within `bytes` of `base`; past them they give zeros.
-struct Window {
-    __amdgpu_buffer_rsrc_t rsrc;
-    __device__ __forceinline__ Window(const void* base, int64_t bytes)
-        : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, static_cast<int>(min<int64_t>(max<int64_t>(bytes, 0), 0xFFFFFFFF)),
-                                                 0x00027000)) {}
-    __device__ __forceinline__ u32x4_t four(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0); }
-    __device__ __forceinline__ uint32_t word(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0); }
-    __device__ __forceinline__ uint32_t two_bytes(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0); }
-    __device__ __forceinline__ uint32_t byte(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b8(rsrc, at, 0, 0); }
-};
-
 // Which tile and which split of the terms a workgroup takes.  Workgroups go to the eight XCDs in turn: each
 // takes a run of tiles of its own, in strips of 8 tiles of right-hand sides, so that what its L2 holds is used
 // by several of them.
@@ -41,9 +20,19 @@ __device__ __forceinline__ TilePlace tile_place(int64_t tiles_i, int64_t tiles_j
     const int64_t total = tiles_i * tiles_j, base = total / 8, rest = total % 8;
     int64_t id = blockIdx.x % total;
     const int64_t x = id % 8;
-    id = x * base + min(x, rest) + id / 8;
-    const int64_t strip = id / (8 * tiles_j), in = id % (8 * tiles_j), high = min<int64_t>(8, tiles_i - strip * 8);
+    id = x * base + lesser(x, rest) + id / 8;
+    const int64_t strip = id / (8 * tiles_j), in = id % (8 * tiles_j), high = lesser(8, tiles_i - strip * 8);
     return {strip * 8 + in % high, in / high, blockIdx.x / total};
+}
+
+// Shared memory, as counted: a 16-byte read serves sixteen lanes at once out of 256 bytes, lanes 0-3, 12-15 and
+// 20-27 together (then 4-11, 16-19 and 28-31, and so for the upper half); a 16-byte write serves eight
+// neighbours out of 128 bytes.  Operands are read with lane (li, lk) on row li: rows 0-3 and 12-15 of one lk meet
+// rows 4-11 of the next.  Where those two pieces of a row differ in one bit, pieces are exchanged by row
+// groups of four in the order 0, 2, 3, 1, which keeps either set of rows within pairs of that bit.
+__device__ __forceinline__ int row_group(int row) {
+    const int g = (row >> 2) & 3;
+    return ((g ^ (g >> 1)) & 1) << 1 | g >> 1;
 }
 
 // How many right-hand sides and results a tile has, and how many workgroups share its sum.

@@ -57,6 +57,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     __shared__ __attribute__((aligned(16))) char Ps[BI * kPRow];
     __shared__ __attribute__((aligned(16))) char Qs[kQRows * kQRow];
     __shared__ uint32_t Ss[TRANS ? 1 : BJ];
+    static_assert(BJ >= 128, "the swizzle of transposed reads");
     static_assert(kQLoads >= 1 && kQRows * kQPieces % kThreads == 0, "codes must split evenly over the threads");
 
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     // what this thread loads of a step: byte offsets in the tile's rows
     const uint32_t p_at = static_cast<uint32_t>(tid / kPChunks * g.pitch * 2 + tid % kPChunks * 16);
     const uint32_t q_at = static_cast<uint32_t>(tid / kQPieces * a.A.ldc + tid % kQPieces * 16);
-    const uint32_t s_at = static_cast<uint32_t>(TRANS ? tid / kQPieces * a.A.lds + tid % kQPieces * 4 / BITS : min(tid, BJ - 1) * a.A.lds);
+    const uint32_t s_at = static_cast<uint32_t>(TRANS ? tid / kQPieces * a.A.lds + tid % kQPieces * 4 / BITS : lesser(tid, BJ - 1) * a.A.lds);
     u32x4_t p_next[kPLoads], q_next[kQLoads];
     uint32_t s_next[kSLoads];
     const auto fetch = [&](int64_t t) {
@@ -104,33 +105,44 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
             }
         }
     };
+    // two rows of P fill the banks; a lane's pieces are 2 lk + u, or 4 u + lk
+    const auto p_swizzle = [](int row) { return TRANS ? (row >> 1) & 7 : row_group(row) << 1 | ((row >> 1) & 1); };
     const auto stage = [&] {
 #pragma unroll
         for (int l = 0; l < kPLoads; ++l) {
             const int id_ = tid + l * kThreads, row = id_ / kPChunks, c = id_ % kPChunks;
-            *reinterpret_cast<u32x4_t*>(Ps + row * kPRow + (c ^ ((row >> 1) & 7)) * 16) = p_next[l];
+            *reinterpret_cast<u32x4_t*>(Ps + row * kPRow + (c ^ p_swizzle(row)) * 16) = p_next[l];
         }
 #pragma unroll
         for (int l = 0; l < kQLoads; ++l) {
             const int id_ = tid + l * kThreads, row = id_ / kQPieces, c = id_ % kQPieces;
             char* to = Qs + row * kQRow;
             if constexpr (!TRANS) {
-                const int at = BITS == 4 ? c ^ ((row >> 3) & 1) : (c + (row >> 2)) & 3;
+                const int at = BITS == 4 ? c ^ ((row >> 3) & 1) : c ^ row_group(row);
                 *reinterpret_cast<u32x4_t*>(to + at * 16) = q_next[l];
             } else {
                 const float s = mx_scale(s_next[l]);
-                const int f = BJ >= 128 ? (row & 3) | ((row >> 1) & 4) : ((row >> 1) & 1) | ((row >> 2) & 2);
+                const int f = (row & 3) | (((row >> 3) ^ (row >> 4)) & 1) << 2;
+                // a lane's pieces of eight values in an order of its own, so that eight neighbours write 128 bytes of banks
+                const int turn = BITS == 4 ? (c >> 1) & 3 : (c >> 2) & 1;
+                u32x4_t w = q_next[l];
+                if constexpr (BITS == 4) {
+                    w = turn & 1 ? u32x4_t{w[1], w[0], w[3], w[2]} : w;
+                    w = turn & 2 ? u32x4_t{w[2], w[3], w[0], w[1]} : w;
+                } else {
+                    w = turn ? u32x4_t{w[2], w[3], w[0], w[1]} : w;
+                }
 #pragma unroll
                 for (int e = 0; e < 16 / BITS; ++e) {
                     u32x4_t v;
-                    if constexpr (BITS == 4) {
-                        const uint32_t w = q_next[l][e];
-                        v = u32x4_t{mx_pair_bf16<4, 0>(w, s), mx_pair_bf16<4, 1>(w, s), mx_pair_bf16<4, 2>(w, s), mx_pair_bf16<4, 3>(w, s)};
-                    } else {
-                        const uint32_t w0 = q_next[l][2 * e], w1 = q_next[l][2 * e + 1];
-                        v = u32x4_t{mx_pair_bf16<8, 0>(w0, s), mx_pair_bf16<8, 1>(w0, s), mx_pair_bf16<8, 0>(w1, s), mx_pair_bf16<8, 1>(w1, s)};
-                    }
-                    *reinterpret_cast<u32x4_t*>(to + ((c * (8 / BITS) + e / 2) ^ f) * 32 + (e & 1) * 16) = v;
+                    if constexpr (BITS == 4)
+                        v = u32x4_t{mx_pair_bf16<4, 0>(w[e], s), mx_pair_bf16<4, 1>(w[e], s), mx_pair_bf16<4, 2>(w[e], s),
+                                    mx_pair_bf16<4, 3>(w[e], s)};
+                    else
+                        v = u32x4_t{mx_pair_bf16<8, 0>(w[2 * e], s), mx_pair_bf16<8, 1>(w[2 * e], s), mx_pair_bf16<8, 0>(w[2 * e + 1], s),
+                                    mx_pair_bf16<8, 1>(w[2 * e + 1], s)};
+                    const int at = e ^ turn;
+                    *reinterpret_cast<u32x4_t*>(to + ((c * (8 / BITS) + at / 2) ^ f) * 32 + (at & 1) * 16) = v;
                 }
             }
         }
@@ -151,11 +163,11 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
                     const u32x2_t c = *reinterpret_cast<const u32x2_t*>(Qs + row * kQRow + ((lk >> 1) ^ ((row >> 3) & 1)) * 16 + (lk & 1) * 8);
                     code[y] = u32x4_t{c[0], c[1], 0u, 0u};
                 } else {
-                    code[y] = *reinterpret_cast<const u32x4_t*>(Qs + row * kQRow + ((lk + (row >> 2)) & 3) * 16);
+                    code[y] = *reinterpret_cast<const u32x4_t*>(Qs + row * kQRow + (lk ^ row_group(row)) * 16);
                 }
             }
         }
-        const int f = BJ >= 128 ? ((li >> 2) & 3) | ((lk & 1) << 2) : ((li >> 3) & 1) | ((lk & 1) << 1);
+        const int f = (li >> 2) | ((lk ^ (lk >> 1)) & 1) << 2;
         const char* qrow = Qs + (8 * lk + (li >> 2)) * kQRow + (li & 3) * 8;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -163,7 +175,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
 #pragma unroll
             for (int x = 0; x < TI; ++x) {
                 const int row = wi + 16 * x + li, c = TRANS ? 4 * u + lk : 2 * lk + u;
-                pv[x] = *reinterpret_cast<const bf16x8*>(Ps + row * kPRow + (c ^ ((row >> 1) & 7)) * 16);
+                pv[x] = *reinterpret_cast<const bf16x8*>(Ps + row * kPRow + (c ^ p_swizzle(row)) * 16);
             }
 #pragma unroll
             for (int y = 0; y < TJ; ++y) {
@@ -211,13 +223,13 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     };
 
     int64_t t = split * g.per;
-    const int64_t t1 = min(t + g.per, g.steps * g.planes);
+    const int64_t t1 = lesser(t + g.per, g.steps * g.planes);
     if (t < t1) {
         fetch(t);
         stage();
     }
     for (bool first = true;; first = false) {
-        const int64_t end = g.flush ? min(t + g.flush, t1) : t1;
+        const int64_t end = g.flush ? lesser(t + g.flush, t1) : t1;
         for (; t < end; ++t) {
             __syncthreads();
             if (t + 1 < t1) fetch(t + 1);
