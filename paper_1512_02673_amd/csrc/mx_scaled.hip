@@ -22,10 +22,10 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 constexpr int kStep = 128;   // terms: four blocks
 
 struct ScaledArgs {
-    int64_t steps, per;
-    float* part;
-    int64_t tiles_i, tiles_j;
-    int32_t flush;
+    int64_t steps;
+    Cut cut;
+    float* part;     // sums of the shared tiles' splits, or null
+    int32_t flush;   // as in mx_tiled.hip
 };
 
 // The rows of codes and scales that one side of a tile takes of a step.
@@ -87,7 +87,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_scaled_kernel(MxArgs a, Scaled
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = (wave & 1) * TI * 16, wj = (wave >> 1) * TJ * 16;
     const int64_t blocks = ceil_div(a.r, kMxBlock);
-    const TilePlace place = tile_place(g.tiles_i, g.tiles_j);
+    const TilePlace place = tile_place(g.cut);
     const int64_t i0 = place.i * BI, j0 = place.j * BJ;
 
     PX px;
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_scaled_kernel(MxArgs a, Scaled
                                   : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(xv[x], av, acc[x][y], kE2M1, kE2M1, 0, xe[x], 0, ae);
         }
     };
-    float* part = g.part ? g.part + place.split * a.s * a.q : nullptr;
+    float* part = place.split < 0 ? nullptr : g.part + (place.split * g.cut.rest() + place.shared) * (BI * BJ);
     // as in mx_tile_kernel
     const auto put = [&](bool first) {
         int at = tid;
@@ -122,8 +122,11 @@ __global__ __launch_bounds__(kThreads, 2) void mx_scaled_kernel(MxArgs a, Scaled
         for (int x = 0; x < TI; ++x)
 #pragma unroll
             for (int y = 0; y < TJ; ++y) {
-                const int64_t i = i0 + wi + 16 * x + (YROWS ? l15 : l4), j = j0 + wj + 16 * y + (YROWS ? l4 : l15);
-                store_four<YROWS>(a, part, a.q, i, j, acc[x][y], first);
+                const int ti = wi + 16 * x + (YROWS ? l15 : l4), tj = wj + 16 * y + (YROWS ? l4 : l15);
+                if (part)
+                    *reinterpret_cast<f32x4_t*>(part + (YROWS ? ti * BJ + tj : tj * BI + ti)) = acc[x][y];
+                else
+                    store_four<YROWS>(a, a.q, i0 + ti, j0 + tj, acc[x][y], first);
                 acc[x][y] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
     };
@@ -136,14 +139,14 @@ __global__ __launch_bounds__(kThreads, 2) void mx_scaled_kernel(MxArgs a, Scaled
         pa.stage(As, Ae);
     };
 
-    int64_t t = place.split * g.per;
-    const int64_t t1 = lesser(t + g.per, g.steps);
+    int64_t t = place.split < 0 ? 0 : place.split * g.cut.per;
+    const int64_t t1 = place.split < 0 ? g.steps : lesser(t + g.cut.per, g.steps);
     if (t < t1) {
         fetch(t);
         stage();
     }
     for (bool first = true;; first = false) {
-        const int64_t end = g.flush ? lesser(t + g.flush, t1) : t1;
+        const int64_t end = g.flush && !part ? lesser(t + g.flush, t1) : t1;
         for (; t < end; ++t) {
             __syncthreads();
             if (t + 1 < t1) fetch(t + 1);
@@ -167,27 +170,24 @@ bool mx_scaled_serves(const MxArgs& a) {
 }
 
 int64_t mx_scaled_workspace_bytes(const MxArgs& a) {
-    const Cut c = cut_of(a);
-    return c.splits > 1 ? c.splits * a.s * a.q * 4 : 0;
+    return cut_of(a).part_bytes();
 }
 
 hipError_t launch_mx_scaled(const MxArgs& a, hipStream_t st) {
     const Cut c = cut_of(a);
     ScaledArgs g{};
     g.steps = ceil_div(a.r, kStep);
-    g.per = c.per;
+    g.cut = c;
     g.part = c.splits > 1 ? static_cast<float*>(a.workspace) : nullptr;
-    g.tiles_i = c.tiles_i;
-    g.tiles_j = c.tiles_j;
-    g.flush = a.y_bf16 || g.part ? 0 : 8192 / kStep;
-    if (!grid_fits(c.tiles_i * c.tiles_j * c.splits, kThreads)) return hipErrorInvalidConfiguration;
-    const dim3 grid(static_cast<uint32_t>(c.tiles_i * c.tiles_j * c.splits));
+    g.flush = a.y_bf16 ? 0 : 16384 / kStep;
+    if (!grid_fits(c.groups(), kThreads)) return hipErrorInvalidConfiguration;
+    const dim3 grid(static_cast<uint32_t>(c.groups()));
     const auto kernel = c.large ? (a.y_rows ? mx_scaled_kernel<4, 8, true> : mx_scaled_kernel<4, 8, false>)
                                 : (a.y_rows ? mx_scaled_kernel<2, 4, true> : mx_scaled_kernel<2, 4, false>);
     kernel<<<grid, kThreads, 0, st>>>(a, g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !g.part) return e;
-    return launch_mx_join(a, g.part, c.splits, a.q, st);
+    return launch_shared_tiles(a, c, g.part, a.q, st);
 }
 
 }  // namespace coded

@@ -10,19 +10,61 @@ namespace coded {
 namespace {
 
 constexpr int kThreads = 256;   // of a tile's workgroup: two waves along each of its sides
-// Which tile and which split of the terms a workgroup takes.  Workgroups go to the eight XCDs in turn: each
-// takes a run of tiles of its own, in strips of 8 tiles of right-hand sides, so that what its L2 holds is used
-// by several of them.
-struct TilePlace {
-    int64_t i, j, split;
+// How many right-hand sides and results a tile has, and which tiles' sums are shared by several workgroups: the
+// first `whole` tiles are one workgroup's each, the rest are split along the terms.
+struct Cut {
+    bool large;                        // 128 x 256, else 64 x 128
+    int64_t tiles_i, tiles_j, whole;
+    int64_t splits, per;               // of each of the other tiles, and steps of a split
+    __host__ __device__ int64_t rest() const { return tiles_i * tiles_j - whole; }
+    __host__ __device__ int64_t groups() const { return whole + rest() * splits; }
+    // fp32 sums of every split of every shared tile, [split][tile][place in the tile, as Y is ordered]
+    int64_t part_bytes() const { return splits > 1 ? rest() * splits * (large ? 128 * 256 : 64 * 128) * 4 : 0; }
 };
-__device__ __forceinline__ TilePlace tile_place(int64_t tiles_i, int64_t tiles_j) {
-    const int64_t total = tiles_i * tiles_j, base = total / 8, rest = total % 8;
-    int64_t id = blockIdx.x % total;
-    const int64_t x = id % 8;
-    id = x * base + lesser(x, rest) + id / 8;
-    const int64_t strip = id / (8 * tiles_j), in = id % (8 * tiles_j), high = lesser(8, tiles_i - strip * 8);
-    return {strip * 8 + in % high, in / high, blockIdx.x / total};
+// 512 large tiles run at once.  What is left over from whole rounds of them would take as long as a round (2112
+// tiles: five rounds for the work of 4.1), so it is split until it fills one, in eight steps a workgroup or more.
+// Fewer than half a round of large tiles are cut into small ones, and those split if they are few.
+inline Cut cut_tiles(int64_t s, int64_t n, int64_t steps) {
+    Cut c{};
+    const int64_t large = ceil_div(s, 128) * ceil_div(n, 256);
+    c.large = large >= 256;
+    c.tiles_i = ceil_div(s, c.large ? 128 : 64);
+    c.tiles_j = ceil_div(n, c.large ? 256 : 128);
+    const int64_t tiles = c.tiles_i * c.tiles_j;
+    c.whole = c.large ? tiles / 512 * 512 : 0;
+    const int64_t rest = tiles - c.whole, want = rest > 0 ? 512 / rest : 0, most = steps / (c.large ? 8 : 4);
+    c.splits = want < most ? want : most;
+    if (c.splits > 16 && c.large) c.splits = 16;
+    if (c.splits < 2) {
+        c.whole = tiles;
+        c.splits = 1;
+    }
+    c.per = steps > 0 ? ceil_div(steps, c.splits) : 1;
+    if (c.splits > 1) c.splits = ceil_div(steps, c.per);
+    return c;
+}
+
+// Which tile a workgroup takes, and which split of its terms (-1: all of them).  Workgroups go to the eight XCDs in
+// turn: of the whole tiles each takes a run of its own, in strips of 8 tiles of right-hand sides, so that what
+// its L2 holds is used by several of them.
+struct TilePlace {
+    int64_t i, j, split, shared;   // shared: its number among the tiles that are split
+};
+__device__ __forceinline__ TilePlace place_of(const Cut& c, int64_t id) {
+    const int64_t strip = id / (8 * c.tiles_j), in = id % (8 * c.tiles_j), high = lesser(8, c.tiles_i - strip * 8);
+    return {strip * 8 + in % high, in / high, -1, 0};
+}
+__device__ __forceinline__ TilePlace tile_place(const Cut& c) {
+    const int64_t b = blockIdx.x;
+    if (b >= c.whole) {
+        const int64_t rest = c.rest(), r = b - c.whole;
+        TilePlace p = place_of(c, c.whole + r % rest);
+        p.split = r / rest;
+        p.shared = r % rest;
+        return p;
+    }
+    const int64_t base = c.whole / 8, more = c.whole % 8, x = b % 8;
+    return place_of(c, x * base + lesser(x, more) + b / 8);
 }
 
 // Shared memory, as counted: a 16-byte read serves sixteen lanes at once out of 256 bytes, lanes 0-3, 12-15 and
@@ -35,34 +77,11 @@ __device__ __forceinline__ int row_group(int row) {
     return ((g ^ (g >> 1)) & 1) << 1 | g >> 1;
 }
 
-// How many right-hand sides and results a tile has, and how many workgroups share its sum.
-struct Cut {
-    bool large;          // 128 x 256, else 64 x 128
-    int64_t tiles_i, tiles_j, per, splits;   // per: steps of a split
-};
-inline Cut cut_tiles(int64_t s, int64_t n, int64_t steps) {
-    Cut c{};
-    c.large = ceil_div(s, 128) * ceil_div(n, 256) >= 256;
-    c.tiles_i = ceil_div(s, c.large ? 128 : 64);
-    c.tiles_j = ceil_div(n, c.large ? 256 : 128);
-    const int64_t want = 512 / (c.tiles_i * c.tiles_j), most = steps / 4;
-    c.splits = c.large || want < 2 || most < 2 ? 1 : want < most ? want : most;
-    c.per = steps > 0 ? ceil_div(steps, c.splits) : 1;
-    c.splits = steps > 0 ? ceil_div(steps, c.per) : 1;
-    return c;
-}
-
 // A result's tile of four: results j .. j + 3 of side i (YROWS), or result j of sides i .. i + 3.
 template <bool YROWS>
-__device__ __forceinline__ void store_four(const MxArgs& a, float* part, int64_t n, int64_t i, int64_t j, f32x4_t v, bool first) {
-    const int64_t side = i, have = YROWS ? n - j : a.s - i;
+__device__ __forceinline__ void store_four(const MxArgs& a, int64_t n, int64_t i, int64_t j, f32x4_t v, bool first) {
+    const int64_t have = YROWS ? n - j : a.s - i;
     if (have <= 0 || (YROWS ? i >= a.s : j >= n)) return;
-    if (part) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < have) part[YROWS ? side * n + j + e : (side + e) * n + j] = v[e];
-        return;
-    }
     const int64_t at = YROWS ? i * a.ldy + j : j * a.ldy + i, ct = YROWS ? i * a.ldcc + j : j * a.ldcc + i;
     v *= a.alpha;
     if (a.C && first) {
@@ -99,6 +118,29 @@ __device__ __forceinline__ void store_four(const MxArgs& a, float* part, int64_t
                 if (e < have) y[e] = first ? v[e] : y[e] + v[e];
         }
     }
+}
+
+// The shared tiles' results from the sums of their splits, added in order.  A workgroup takes 1024 places of a tile.
+template <int BI, int BJ, bool YROWS>
+__global__ __launch_bounds__(kThreads) void mx_shared_tiles_kernel(MxArgs a, Cut c, const float* part, int64_t n) {
+    constexpr int kParts = BI * BJ / (4 * kThreads);
+    const int64_t tile = blockIdx.x / kParts;
+    const int at = (static_cast<int>(blockIdx.x % kParts) * kThreads + threadIdx.x) * 4;
+    const TilePlace p = place_of(c, c.whole + tile);
+    const float* from = part + tile * (BI * BJ) + at;
+    f32x4_t v = *reinterpret_cast<const f32x4_t*>(from);
+    for (int64_t k = 1; k < c.splits; ++k) v += *reinterpret_cast<const f32x4_t*>(from + k * c.rest() * (BI * BJ));
+    const int64_t i = p.i * BI + (YROWS ? at / BJ : at % BI), j = p.j * BJ + (YROWS ? at % BJ : at / BI);
+    store_four<YROWS>(a, n, i, j, v, true);
+}
+
+inline hipError_t launch_shared_tiles(const MxArgs& a, const Cut& c, const float* part, int64_t n, hipStream_t st) {
+    const int64_t blocks = c.rest() * ((c.large ? 128 * 256 : 64 * 128) / (4 * kThreads));
+    if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
+    const auto kernel = c.large ? (a.y_rows ? mx_shared_tiles_kernel<128, 256, true> : mx_shared_tiles_kernel<128, 256, false>)
+                                : (a.y_rows ? mx_shared_tiles_kernel<64, 128, true> : mx_shared_tiles_kernel<64, 128, false>);
+    kernel<<<dim3(static_cast<uint32_t>(blocks)), kThreads, 0, st>>>(a, c, part, n);
+    return hipGetLastError();
 }
 
 }  // namespace

@@ -26,13 +26,11 @@ constexpr int kStep = 64;   // terms
 struct TileArgs {
     const uint16_t* P;
     int64_t pitch, plane;       // elements between rows, and between planes
-    int64_t row;                // elements of a row that are there: whole steps
+    int64_t row;                // elements of a row that are there: whole steps (by columns: rows)
     int32_t planes;
     int64_t steps;              // of one plane
-    int64_t per;                // steps of a split
-    int64_t splits;
-    float* part;                // sums of each split [split][side][result], or null
-    int64_t tiles_i, tiles_j;
+    Cut cut;
+    float* part;                // sums of the shared tiles' splits, or null
     int32_t flush;              // steps summed in one chain (fp32 results), 0: all
 };
 
@@ -44,11 +42,14 @@ struct TileArgs {
 // comes before shared memory, which holds rows of bf16 values; the operands,
 // eight terms of a column, are read transposed.  Lane (li, lk) takes terms 8 lk
 // .. 8 lk + 7 of each 32.
-template <int BITS, bool TRANS, int TI, int TJ, bool YROWS>
+//
+// X by columns (PT: a row of X holds one term of every right-hand side) lies in
+// shared memory as it is in memory, and its operands are read transposed too.
+template <int BITS, bool TRANS, bool PT, int TI, int TJ, bool YROWS>
 __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs g) {
     constexpr int BI = 32 * TI, BJ = 32 * TJ;
-    constexpr int kPRow = kStep * 2, kPChunks = kPRow / 16;          // bytes and 16-byte pieces of a row of P
-    constexpr int kPLoads = BI * kPChunks / kThreads;
+    constexpr int kPRow = PT ? BI * 2 : kStep * 2, kPChunks = kPRow / 16;   // bytes and 16-byte pieces of a row of P's tile
+    constexpr int kPLoads = BI * kStep * 2 / 16 / kThreads;
     constexpr int kQRow = TRANS ? BJ * 2 : kStep * BITS / 8;         // shared memory: [k][j] in bf16, or [j] codes
     constexpr int kQRows = TRANS ? kStep : BJ;
     constexpr int kQPieces = TRANS ? BJ * BITS / 8 / 16 : kQRow / 16;   // 16-byte pieces of codes in a row of the tile
@@ -57,7 +58,6 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     __shared__ __attribute__((aligned(16))) char Ps[BI * kPRow];
     __shared__ __attribute__((aligned(16))) char Qs[kQRows * kQRow];
     __shared__ uint32_t Ss[TRANS ? 1 : BJ];
-    static_assert(BJ >= 128, "the swizzle of transposed reads");
     static_assert(kQLoads >= 1 && kQRows * kQPieces % kThreads == 0, "codes must split evenly over the threads");
 
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
@@ -66,8 +66,8 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     const int64_t n = TRANS ? a.r : a.q;
     const int64_t blocks = ceil_div(a.r, kMxBlock), code_row = blocks * 4 * BITS;
 
-    const TilePlace place = tile_place(g.tiles_i, g.tiles_j);
-    const int64_t split = place.split, i0 = place.i * BI, j0 = place.j * BJ;
+    const TilePlace place = tile_place(g.cut);
+    const int64_t i0 = place.i * BI, j0 = place.j * BJ;
 
     // what this thread loads of a step: byte offsets in the tile's rows
     const uint32_t p_at = static_cast<uint32_t>(tid / kPChunks * g.pitch * 2 + tid % kPChunks * 16);
@@ -75,35 +75,69 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     const uint32_t s_at = static_cast<uint32_t>(TRANS ? tid / kQPieces * a.A.lds + tid % kQPieces * 4 / BITS : lesser(tid, BJ - 1) * a.A.lds);
     u32x4_t p_next[kPLoads], q_next[kQLoads];
     uint32_t s_next[kSLoads];
-    const auto fetch = [&](int64_t t) {
-        const int64_t h = t / g.steps, k0 = (t - h * g.steps) * kStep;
-        const Window p(g.P + h * g.plane + i0 * g.pitch + k0, ((a.s - i0 - 1) * g.pitch + g.row - k0) * 2);
+    // The next step to load: where its operands begin, the bytes from there on, and its number in its plane.
+    // They move on from step to step (multiplied out anew, the scalar unit's work was as long as the matrix cores').
+    const int64_t t0 = place.split < 0 ? 0 : place.split * g.cut.per;
+    int64_t step = t0 > 0 ? t0 % g.steps : 0;
+    const int64_t q_step = TRANS ? kStep * a.A.ldc : kStep * BITS / 8, s_step = TRANS ? kStep * a.A.lds : kStep / kMxBlock;
+    const int64_t q_skip = TRANS ? j0 * BITS / 8 : j0 * a.A.ldc, s_skip = TRANS ? j0 / kMxBlock : j0 * a.A.lds;
+    const int64_t q_all = (a.q - 1) * a.A.ldc + code_row - q_skip;
+    const int64_t s_all = (a.q - 1) * a.A.lds + (TRANS ? blocks : ceil_div(blocks, 4) * 4) - s_skip;
+    const int64_t plane = t0 > 0 ? t0 / g.steps : 0, p_step = PT ? kStep * g.pitch : kStep;
+    const uint16_t* p_base = g.P + plane * g.plane + (PT ? i0 : i0 * g.pitch) + step * p_step;
+    const int64_t p_all = PT ? (g.row - 1) * g.pitch + a.s - i0 : (a.s - i0 - 1) * g.pitch + g.row;
+    int64_t p_left = (p_all - step * p_step) * 2;
+    const uint8_t *q_base = a.A.codes + q_skip + step * q_step, *s_base = a.A.scales + s_skip + step * s_step;
+    int64_t q_left = q_all - step * q_step, s_left = s_all - step * s_step;
+    const auto fetch = [&] {
+        const Window p(p_base, p_left), q(q_base, q_left), s(s_base, s_left);
 #pragma unroll
         for (int l = 0; l < kPLoads; ++l) p_next[l] = p.four(p_at + static_cast<uint32_t>(l * (kThreads / kPChunks) * 2 * g.pitch));
+#pragma unroll
+        for (int l = 0; l < kQLoads; ++l) q_next[l] = q.four(q_at + static_cast<uint32_t>(l * (kThreads / kQPieces) * a.A.ldc));
         if constexpr (TRANS) {
             // rows past q are zeros; columns past r are other bytes within A, and are not stored
-            const int64_t c0 = j0 * BITS / 8, b0 = j0 / kMxBlock;
-            const Window q(a.A.codes + k0 * a.A.ldc + c0, (a.q - k0 - 1) * a.A.ldc + code_row - c0);
-            const Window s(a.A.scales + k0 * a.A.lds + b0, (a.q - k0 - 1) * a.A.lds + blocks - b0);
 #pragma unroll
-            for (int l = 0; l < kQLoads; ++l) {
-                q_next[l] = q.four(q_at + static_cast<uint32_t>(l * (kThreads / kQPieces) * a.A.ldc));
-                s_next[l] = s.byte(s_at + static_cast<uint32_t>(l * (kThreads / kQPieces) * a.A.lds));
-            }
+            for (int l = 0; l < kQLoads; ++l) s_next[l] = s.byte(s_at + static_cast<uint32_t>(l * (kThreads / kQPieces) * a.A.lds));
         } else {
-            const int64_t c0 = k0 * BITS / 8, b0 = k0 / kMxBlock;
-            const Window q(a.A.codes + j0 * a.A.ldc + c0, (a.q - j0 - 1) * a.A.ldc + code_row - c0);
-            const Window s(a.A.scales + j0 * a.A.lds + b0, (a.q - j0 - 1) * a.A.lds + ceil_div(blocks, 4) * 4 - b0);
-#pragma unroll
-            for (int l = 0; l < kQLoads; ++l) q_next[l] = q.four(q_at + static_cast<uint32_t>(l * (kThreads / kQPieces) * a.A.ldc));
             s_next[0] = s.two_bytes(s_at);
-            if (k0 + kStep > blocks * kMxBlock) {   // one block left: what lies behind a row is not a number for sure
+            if (step * kStep + kStep > blocks * kMxBlock) {   // one block left: what lies behind a row is not a number for sure
                 s_next[0] &= 0xFFu;
                 if (tid % kQPieces >= kQPieces / 2)
 #pragma unroll
                     for (int l = 0; l < kQLoads; ++l) q_next[l] = u32x4_t{0u, 0u, 0u, 0u};
             }
         }
+        p_base += p_step;
+        p_left -= p_step * 2;
+        q_base += q_step;
+        q_left -= q_step;
+        s_base += s_step;
+        s_left -= s_step;
+        if (++step == g.steps) {   // the next plane
+            p_base += g.plane - g.steps * p_step;
+            p_left = p_all * 2;
+            q_base -= g.steps * q_step;
+            q_left = q_all;
+            s_base -= g.steps * s_step;
+            s_left = s_all;
+            step = 0;
+        }
+    };
+    // Runs of 32 bytes of a row that is read transposed, exchanged so that two neighbouring parts of a wave, four
+    // rows each, read all banks: their rows are 8 (across the blocks) or 16 (along them) apart.  Rows of 128
+    // bytes fill the banks in pairs.
+    const auto run_swizzle = [](int row, int pitch) {
+        const int far = TRANS ? (row >> 3) & 1 : (row >> 4) & 1;
+        return pitch >= 256 ? (row & 3) | far << 2 : ((row >> 1) & 1) | far << 1;
+    };
+    const auto transposed = [&](const char* tile, int pitch, int run, int u) {
+        typedef __attribute__((address_space(3))) s16x4_t lds4;
+        const int row = (TRANS ? 32 * u + 8 * lk : 16 * lk + 8 * u) + (li >> 2);
+        const char* at = tile + row * pitch + (run ^ run_swizzle(row, pitch)) * 32 + (li & 3) * 8;
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(at));
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(at + 4 * pitch));   // the same runs there
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
     // two rows of P fill the banks; a lane's pieces are 2 lk + u, or 4 u + lk
     const auto p_swizzle = [](int row) { return TRANS ? (row >> 1) & 7 : row_group(row) << 1 | ((row >> 1) & 1); };
@@ -111,7 +145,8 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
 #pragma unroll
         for (int l = 0; l < kPLoads; ++l) {
             const int id_ = tid + l * kThreads, row = id_ / kPChunks, c = id_ % kPChunks;
-            *reinterpret_cast<u32x4_t*>(Ps + row * kPRow + (c ^ p_swizzle(row)) * 16) = p_next[l];
+            const int at = !PT ? c ^ p_swizzle(row) : c ^ run_swizzle(row, kPRow) << 1;
+            *reinterpret_cast<u32x4_t*>(Ps + row * kPRow + at * 16) = p_next[l];
         }
 #pragma unroll
         for (int l = 0; l < kQLoads; ++l) {
@@ -122,7 +157,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
                 *reinterpret_cast<u32x4_t*>(to + at * 16) = q_next[l];
             } else {
                 const float s = mx_scale(s_next[l]);
-                const int f = (row & 3) | (((row >> 3) ^ (row >> 4)) & 1) << 2;
+                const int f = run_swizzle(row, kQRow);
                 // a lane's pieces of eight values in an order of its own, so that eight neighbours write 128 bytes of banks
                 const int turn = BITS == 4 ? (c >> 1) & 3 : (c >> 2) & 1;
                 u32x4_t w = q_next[l];
@@ -167,25 +202,22 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
                 }
             }
         }
-        const int f = (li >> 2) | ((lk ^ (lk >> 1)) & 1) << 2;
-        const char* qrow = Qs + (8 * lk + (li >> 2)) * kQRow + (li & 3) * 8;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             bf16x8 pv[TI];
 #pragma unroll
             for (int x = 0; x < TI; ++x) {
                 const int row = wi + 16 * x + li, c = TRANS ? 4 * u + lk : 2 * lk + u;
-                pv[x] = *reinterpret_cast<const bf16x8*>(Ps + row * kPRow + (c ^ p_swizzle(row)) * 16);
+                if constexpr (PT)
+                    pv[x] = transposed(Ps, kPRow, wi / 16 + x, u);
+                else
+                    pv[x] = *reinterpret_cast<const bf16x8*>(Ps + row * kPRow + (c ^ p_swizzle(row)) * 16);
             }
 #pragma unroll
             for (int y = 0; y < TJ; ++y) {
                 bf16x8 qv;
                 if constexpr (TRANS) {
-                    typedef __attribute__((address_space(3))) s16x4_t lds4;
-                    const char* at = qrow + 32 * u * kQRow + ((wj / 16 + y) ^ f) * 32;
-                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(at));
-                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(at + 4 * kQRow));
-                    qv = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                    qv = transposed(Qs, kQRow, wj / 16 + y, u);
                 } else {
                     u32x4_t d;
                     if constexpr (BITS == 4) {
@@ -206,7 +238,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
             }
         }
     };
-    float* part = g.part ? g.part + split * a.s * n : nullptr;
+    float* part = place.split < 0 ? nullptr : g.part + (place.split * g.cut.rest() + place.shared) * (BI * BJ);
     // the lane's place in the tile, computed anew each time: kept, its addresses would take registers from the sums
     const auto put = [&](bool first) {
         int at = tid;
@@ -216,23 +248,26 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
         for (int x = 0; x < TI; ++x)
 #pragma unroll
             for (int y = 0; y < TJ; ++y) {
-                const int64_t i = i0 + wi + 16 * x + (YROWS ? l15 : l4), j = j0 + wj + 16 * y + (YROWS ? l4 : l15);
-                store_four<YROWS>(a, part, n, i, j, acc[x][y], first);
+                const int ti = wi + 16 * x + (YROWS ? l15 : l4), tj = wj + 16 * y + (YROWS ? l4 : l15);
+                if (part)
+                    *reinterpret_cast<f32x4_t*>(part + (YROWS ? ti * BJ + tj : tj * BI + ti)) = acc[x][y];
+                else
+                    store_four<YROWS>(a, n, i0 + ti, j0 + tj, acc[x][y], first);
                 acc[x][y] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
     };
 
-    int64_t t = split * g.per;
-    const int64_t t1 = lesser(t + g.per, g.steps * g.planes);
+    int64_t t = t0;
+    const int64_t all = g.steps * g.planes, t1 = place.split < 0 ? all : lesser(t + g.cut.per, all);
     if (t < t1) {
-        fetch(t);
+        fetch();
         stage();
     }
     for (bool first = true;; first = false) {
-        const int64_t end = g.flush ? lesser(t + g.flush, t1) : t1;
+        const int64_t end = g.flush && !part ? lesser(t + g.flush, t1) : t1;
         for (; t < end; ++t) {
             __syncthreads();
-            if (t + 1 < t1) fetch(t + 1);
+            if (t + 1 < t1) fetch();
             compute();
             __syncthreads();
             if (t + 1 < t1) stage();
@@ -292,11 +327,10 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const void* X, int64_t ldx
 
 // How a product is cut up.
 struct Plan {
-    bool pack;          // X goes through the workspace
+    bool pack, by_columns;   // X goes through the workspace; it is taken as it is, a term of every side a row
     int planes;
     int64_t steps, pitch, plane, pack_bytes;
     Cut cut;
-    int64_t part_bytes;
 };
 
 constexpr int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
@@ -309,21 +343,28 @@ Plan make_plan(const MxArgs& a, bool x) {
     p.steps = ceil_div(terms, kStep);
     p.pitch = p.steps * kStep;
     p.plane = a.s * p.pitch;
-    p.pack = !(x && !a.x_bits && a.x_bf16 && a.x_rows && terms % kStep == 0 && a.ldx % 8 == 0 && (reinterpret_cast<uintptr_t>(a.X) & 15) == 0);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(a.X);
+    const bool bf16 = x && !a.x_bits && a.x_bf16;
+    p.by_columns = bf16 && !a.x_rows && a.ldx % 2 == 0 && a.ldx < (int64_t(1) << 31) / 128 && at % 4 == 0;
+    p.pack = !p.by_columns && !(bf16 && a.x_rows && terms % kStep == 0 && a.ldx % 8 == 0 && at % 16 == 0);
     p.pack_bytes = round_up(p.planes * p.plane * 2, 256);
     p.cut = cut_tiles(a.s, n, p.steps * p.planes);
-    p.part_bytes = p.cut.splits > 1 ? p.cut.splits * a.s * n * 4 : 0;
     return p;
 }
 
-template <int BITS, bool TRANS>
+template <int BITS, bool TRANS, bool PT>
 hipError_t launch_tiles(const MxArgs& a, const TileArgs& g, bool large, hipStream_t st) {
-    const dim3 grid(static_cast<uint32_t>(g.tiles_i * g.tiles_j * g.splits));
-    // split sums are laid out as y_rows results are
-    const auto kernel = large ? (a.y_rows ? mx_tile_kernel<BITS, TRANS, 4, 8, true> : mx_tile_kernel<BITS, TRANS, 4, 8, false>)
-                              : (a.y_rows ? mx_tile_kernel<BITS, TRANS, 2, 4, true> : mx_tile_kernel<BITS, TRANS, 2, 4, false>);
+    const dim3 grid(static_cast<uint32_t>(g.cut.groups()));
+    const auto kernel = large ? (a.y_rows ? mx_tile_kernel<BITS, TRANS, PT, 4, 8, true> : mx_tile_kernel<BITS, TRANS, PT, 4, 8, false>)
+                              : (a.y_rows ? mx_tile_kernel<BITS, TRANS, PT, 2, 4, true> : mx_tile_kernel<BITS, TRANS, PT, 2, 4, false>);
     kernel<<<grid, kThreads, 0, st>>>(a, g);
     return hipGetLastError();
+}
+
+template <int BITS>
+hipError_t launch_bits(const MxArgs& a, const TileArgs& g, const Plan& p, hipStream_t st) {
+    if (a.trans) return p.by_columns ? launch_tiles<BITS, true, true>(a, g, p.cut.large, st) : launch_tiles<BITS, true, false>(a, g, p.cut.large, st);
+    return p.by_columns ? launch_tiles<BITS, false, true>(a, g, p.cut.large, st) : launch_tiles<BITS, false, false>(a, g, p.cut.large, st);
 }
 
 }  // namespace
@@ -336,7 +377,7 @@ bool mx_tiled_serves(const MxArgs& a) {
 
 int64_t mx_tiled_workspace_bytes(const MxArgs& a) {
     const Plan p = make_plan(a, false);
-    return p.pack_bytes + p.part_bytes;
+    return p.pack_bytes + p.cut.part_bytes();
 }
 
 hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
@@ -346,16 +387,13 @@ hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
     g.P = p.pack ? static_cast<const uint16_t*>(a.workspace) : static_cast<const uint16_t*>(a.X);
     g.pitch = p.pack ? p.pitch : a.ldx;
     g.plane = p.plane;
-    g.row = p.pitch;
+    g.row = p.by_columns ? terms : p.pitch;
     g.planes = p.planes;
     g.steps = p.steps;
-    g.per = p.cut.per;
-    g.splits = p.cut.splits;
+    g.cut = p.cut;
     g.part = p.cut.splits > 1 ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + p.pack_bytes) : nullptr;
-    g.tiles_i = p.cut.tiles_i;
-    g.tiles_j = p.cut.tiles_j;
-    g.flush = a.y_bf16 || g.part ? 0 : 8192 / kStep;
-    if (!grid_fits(p.cut.tiles_i * p.cut.tiles_j * p.cut.splits, kThreads)) return hipErrorInvalidConfiguration;
+    g.flush = a.y_bf16 ? 0 : 16384 / kStep;
+    if (!grid_fits(p.cut.groups(), kThreads)) return hipErrorInvalidConfiguration;
     if (a.x_bits && p.pitch > 0) {
         const int64_t blocks = ceil_div(a.s * (p.pitch / 8), 256);
         if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
@@ -371,10 +409,9 @@ hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const hipError_t e = a.A.bits == 4 ? (a.trans ? launch_tiles<4, true>(a, g, p.cut.large, st) : launch_tiles<4, false>(a, g, p.cut.large, st))
-                                       : (a.trans ? launch_tiles<8, true>(a, g, p.cut.large, st) : launch_tiles<8, false>(a, g, p.cut.large, st));
+    const hipError_t e = a.A.bits == 4 ? launch_bits<4>(a, g, p, st) : launch_bits<8>(a, g, p, st);
     if (e != hipSuccess || !g.part) return e;
-    return launch_mx_join(a, g.part, g.splits, n, st);
+    return launch_shared_tiles(a, p.cut, g.part, n, st);
 }
 
 }  // namespace coded
