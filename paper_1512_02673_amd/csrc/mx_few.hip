@@ -167,24 +167,27 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
         code_row[x] = row * static_cast<uint32_t>(a.A.ldc);
         scale_row[x] = row * static_cast<uint32_t>(a.A.lds);
     }
-    u32x4_t w[RT][4];
+    // Codes of the next steps are on their way: of two where the registers allow it, else of one.
+    constexpr int D = NT == 1 ? 2 : 1;
+    u32x4_t w[D][RT][4];
     typedef unsigned int scales_t __attribute__((ext_vector_type(kScales)));
-    scales_t sc[RT];
-    const auto fetch = [&](int step) {
+    scales_t sc[D][RT];
+    const auto fetch = [&](int step, auto S) {
+        constexpr int d = S.value % D;
         const int p0 = step * 16 + lk, b0 = step * kScales * 4;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const bool in = p0 + 4 * t < static_cast<int>(pieces_a);
 #pragma unroll
-            for (int x = 0; x < RT; ++x) w[x][t] = codes.four(in ? code_row[x] + (p0 + 4 * t) * 16 : kNowhere);
+            for (int x = 0; x < RT; ++x) w[d][x][t] = codes.four(in ? code_row[x] + (p0 + 4 * t) * 16 : kNowhere);
         }
 #pragma unroll
         for (int x = 0; x < RT; ++x) {
             const uint32_t at = p0 < static_cast<int>(pieces_a) + lk ? scale_row[x] + b0 : kNowhere;   // the step's first piece is in the row
             if constexpr (BITS == 4)
-                sc[x] = scales.four(at);
+                sc[d][x] = scales.four(at);
             else
-                sc[x] = scales.two(at);
+                sc[d][x] = scales.two(at);
         }
     };
 
@@ -194,8 +197,9 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
     const int step_bytes = kStep * pitch * 2;
 
     f32x4_t sum[RT][NT] = {};
-    // a step's sums from X at xs; the next step's codes are on their way before they begin
-    const auto compute = [&](const char* xs, int step, int next) {
+    // a step's sums from X at xs; the codes of the step `next` are on their way before they begin
+    const auto compute = [&](const char* xs, int step, int next, auto S) {
+        constexpr int d = S.value % D;
         u32x4_t cw[RT][4];
         float scale[RT][4];
         const int left = static_cast<int>(blocks) - step * kScales * 4;
@@ -203,18 +207,18 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
 #pragma unroll
             for (int i = 0; i < kScales; ++i)
 #pragma unroll
-                for (int x = 0; x < RT; ++x) sc[x][i] &= left >= 4 * i + 4 ? ~0u : left <= 4 * i ? 0u : (1u << (8 * (left - 4 * i))) - 1;
+                for (int x = 0; x < RT; ++x) sc[d][x][i] &= left >= 4 * i + 4 ? ~0u : left <= 4 * i ? 0u : (1u << (8 * (left - 4 * i))) - 1;
         }
 #pragma unroll
         for (int x = 0; x < RT; ++x)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                cw[x][t] = w[x][t];
+                cw[x][t] = w[d][x][t];
                 // piece 4 t + lk: byte lk of word t, or (two pieces a block) byte 2 t + lk / 2
-                const uint32_t byte = BITS == 4 ? sc[x][t] >> (8 * lk) : sc[x][t / 2] >> (16 * (t & 1) + 8 * (lk >> 1));
+                const uint32_t byte = BITS == 4 ? sc[d][x][t] >> (8 * lk) : sc[d][x][t / 2] >> (16 * (t & 1) + 8 * (lk >> 1));
                 scale[x][t] = mx_scale(byte & 0xFFu);
             }
-        fetch(next);
+        fetch(next, S);
         f32x4_t acc[RT][NT] = {};
         // X's operands are read one part ahead
         bf16x8 xv[2][NT];
@@ -245,8 +249,13 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
     // Rounds of one step of each of the WK waves.  Workgroups start at different ones: in step, they would all
     // read the same columns of their rows, a whole row apart.
     const int rounds = static_cast<int>(ceil_div(steps, WK)), none = static_cast<int>(steps) + WK;
-    int c = blockIdx.x % rounds;
-    fetch(c * WK + wk);
+    const int first = blockIdx.x % rounds;
+    const auto round_at = [&](int i) { return first + i < rounds ? first + i : first + i - rounds; };   // i <= rounds
+    const auto step_at = [&](int i) { return i < rounds ? round_at(i) * WK + wk : none; };
+    typedef std::integral_constant<int, 0> even;
+    typedef std::integral_constant<int, 1> odd;
+    fetch(step_at(0), even{});
+    if constexpr (D == 2) fetch(step_at(1), odd{});
     if constexpr (COLS) {
         const int round = WK * step_bytes;
         const Window x(image, steps * step_bytes);
@@ -259,17 +268,17 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
 #pragma unroll
             for (int i = 0; i < CP; ++i) *reinterpret_cast<u32x4_t*>(to + (tid + i * kThreads) * 16) = xr[i];
         };
-        copy_in(c);
+        copy_in(first);
         copy_out(smem);
-        int half = 0;
-        for (int i = 0; i < rounds; ++i) {
+        const auto turn = [&](int i, auto S) {
             __syncthreads();
-            const int next = c + 1 < rounds ? c + 1 : 0;
-            copy_in(next);
-            compute(smem + half * round + wk * step_bytes, c * WK + wk, i + 1 < rounds ? next * WK + wk : none);
-            c = next;
-            half ^= 1;
-            copy_out(smem + half * round);
+            copy_in(round_at(i + 1));
+            compute(smem + S.value * round + wk * step_bytes, step_at(i), step_at(i + D), S);
+            copy_out(smem + (1 - S.value) * round);
+        };
+        for (int i = 0; i < rounds; i += 2) {
+            turn(i, even{});
+            if (i + 1 < rounds) turn(i + 1, odd{});
         }
     } else {
         const int pieces = static_cast<int>(steps) * (kStep / 8);
@@ -281,14 +290,16 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
             for (int h = 0; h < planes; ++h) *reinterpret_cast<u32x4_t*>(to + h * s * 16) = h == 0 ? v[0] : h == 1 ? v[1] : v[2];
         }
         __syncthreads();
-        for (int i = 0; i < rounds; ++i) {
-            const int next = c + 1 < rounds ? c + 1 : 0, m = c * WK + wk;
-            const int then = i + 1 < rounds ? next * WK + wk : none;
+        const auto turn = [&](int i, auto S) {
+            const int m = step_at(i);
             if (m < steps)
-                compute(smem + m * step_bytes, m, then);
+                compute(smem + m * step_bytes, m, step_at(i + D), S);
             else
-                fetch(then);
-            c = next;
+                fetch(step_at(i + D), S);
+        };
+        for (int i = 0; i < rounds; i += 2) {
+            turn(i, even{});
+            if (i + 1 < rounds) turn(i + 1, odd{});
         }
     }
 
@@ -332,7 +343,7 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
 // Rows past q repeat the last one and meet zeros of U; columns past r repeat
 // the last block and are not stored.
 template <int BITS, int W>
-__global__ __launch_bounds__(kThreads, 2) void mx_few_t_kernel(MxArgs a, int planes, int64_t per, int rows_staged, int64_t groups,
+__global__ __launch_bounds__(kThreads, W == 16 ? 2 : 4) void mx_few_t_kernel(MxArgs a, int planes, int64_t per, int rows_staged, int64_t groups,
                                                                float* part) {
     constexpr int CW = W * 8 / BITS;   // columns of a lane
     constexpr int kCols = 16 * CW;     // and of a workgroup
@@ -348,7 +359,6 @@ __global__ __launch_bounds__(kThreads, 2) void mx_few_t_kernel(MxArgs a, int pla
     const int s = static_cast<int>(a.s), cols = planes * s;
     const int64_t j0 = group * kCols;
     typedef unsigned int words_t __attribute__((ext_vector_type(W / 4)));
-    static_assert(W == 16, "");
     words_t w[8];
     uint32_t sc[8];
     // rows past q read as zeros; columns past r are other bytes of A, or zeros, and are not stored
@@ -360,7 +370,10 @@ __global__ __launch_bounds__(kThreads, 2) void mx_few_t_kernel(MxArgs a, int pla
         const Window scales(a.A.scales + t * a.A.lds + b0_, have < 0 ? 0 : have * a.A.lds + blocks - b0_);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            w[e] = codes.four(code_at + static_cast<uint32_t>(e * a.A.ldc));
+            if constexpr (W == 16)
+                w[e] = codes.four(code_at + static_cast<uint32_t>(e * a.A.ldc));
+            else
+                w[e] = codes.two(code_at + static_cast<uint32_t>(e * a.A.ldc));
             sc[e] = scales.byte(scale_at + static_cast<uint32_t>(e * a.A.lds));
         }
     };
@@ -420,7 +433,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_few_t_kernel(MxArgs a, int pla
     // another would be a chain of barriers; four columns of every lane at a time
     // keep the waves' tiles within 64 x 65 floats each.
     float* red = reinterpret_cast<float*>(smem);
-    constexpr int kPass = 4;          // columns of a lane a pass
+    constexpr int kPass = 4;   // columns of a lane a pass
     constexpr int kPitch = 16 * kPass + 1;
 #pragma unroll
     for (int n0 = 0; n0 < CW; n0 += kPass) {
@@ -443,6 +456,110 @@ __global__ __launch_bounds__(kThreads, 2) void mx_few_t_kernel(MxArgs a, int pla
                 part[(split * s + c) * a.r + at] = v;
             else
                 mx_store(a, c, at, v);
+        }
+    }
+}
+
+// Z = A^T u for one vector, in fp32 on the vector units.  As above, but each lane
+// adds its 32 (16) columns by itself: a row's codes are used up by themselves, so
+// the same registers take the row 256 further down at once, and with 32 sums
+// instead of 128 twice as many waves have loads under way.  The sums of the four
+// parts of a wave, of the eight waves and of the workgroups are added at the end.
+template <int BITS>
+__global__ __launch_bounds__(kThreads, 4) void mx_vector_t_kernel(MxArgs a, int64_t per, int rows_staged, int64_t groups, float* part) {
+    constexpr int CW = 128 / BITS, kCols = 16 * CW;   // columns of a lane, and of a workgroup
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    float* us = reinterpret_cast<float*>(smem);
+    const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t base = gridDim.x / 8, rest = gridDim.x % 8, xcd = blockIdx.x % 8;   // as in mx_few_t_kernel
+    const int64_t id = xcd * base + lesser(xcd, rest) + blockIdx.x / 8;
+    const int64_t group = id % groups, split = id / groups;
+    const int64_t t0 = split * per, t1 = lesser(t0 + per, a.q), j0 = group * kCols;
+    const int64_t blocks = ceil_div(a.r, kMxBlock), c0_ = j0 * BITS / 8, b0_ = j0 / kMxBlock;
+    const uint32_t code_at = static_cast<uint32_t>(8 * lk * a.A.ldc) + li * 16, scale_at = static_cast<uint32_t>(8 * lk * a.A.lds) + li * CW / kMxBlock;
+    u32x4_t w[8];
+    uint32_t sc[8];
+    const auto codes_of = [&](int64_t t) {
+        const int64_t have = lesser(a.q - t, 32) - 1;
+        return Window(a.A.codes + t * a.A.ldc + c0_, have < 0 ? 0 : have * a.A.ldc + blocks * 4 * BITS - c0_);
+    };
+    const auto scales_of = [&](int64_t t) {
+        const int64_t have = lesser(a.q - t, 32) - 1;
+        return Window(a.A.scales + t * a.A.lds + b0_, have < 0 ? 0 : have * a.A.lds + blocks - b0_);
+    };
+    const auto fetch = [&](const Window& codes, const Window& scales, int e) {
+        w[e] = codes.four(code_at + static_cast<uint32_t>(e * a.A.ldc));
+        sc[e] = scales.byte(scale_at + static_cast<uint32_t>(e * a.A.lds));
+    };
+    float acc[CW] = {};
+    int64_t mine = t0 + wave * 32;
+    {
+        const int64_t t = lesser(mine, a.q);
+        const Window codes = codes_of(t), scales = scales_of(t);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) fetch(codes, scales, e);
+    }
+    for (int64_t c0 = t0; c0 < t1; c0 += rows_staged) {
+        const int64_t end = lesser(c0 + rows_staged, t1);
+        const int rows = static_cast<int>(ceil_div(end - c0, 32) * 32);
+        __syncthreads();
+        for (int i = tid; i < rows; i += kThreads) {
+            const int64_t at = a.x_rows ? c0 + i : (c0 + i) * a.ldx;
+            us[i] = c0 + i >= t1 ? 0.0f
+                    : a.x_bf16   ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(a.X)[at]) << 16)
+                                 : static_cast<const float*>(a.X)[at];
+        }
+        __syncthreads();
+        for (; mine < end; mine += 32 * kWaves) {
+            const f32x4_t* up = reinterpret_cast<const f32x4_t*>(us + static_cast<int>(mine - c0) + 8 * lk);
+            const f32x4_t u[2] = {up[0], up[1]};
+            const int64_t next = mine + 32 * kWaves < t1 ? mine + 32 * kWaves : a.q;
+            const Window codes = codes_of(next), scales = scales_of(next);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float s = mx_scale(sc[e]), f = u[e / 4][e % 4];
+#pragma unroll
+                for (int word = 0; word < 4; ++word) {
+                    const auto pair = [&](auto P) {
+                        const mx_f32x2 v = mx_pair_f32<BITS, P.value>(w[e][word], s);
+                        const int n = word * (32 / BITS) + 2 * P.value;
+                        acc[n] = fmaf(v.x, f, acc[n]);
+                        acc[n + 1] = fmaf(v.y, f, acc[n + 1]);
+                    };
+                    pair(std::integral_constant<int, 0>{});
+                    pair(std::integral_constant<int, 1>{});
+                    if constexpr (BITS == 4) {
+                        pair(std::integral_constant<int, 2>{});
+                        pair(std::integral_constant<int, 3>{});
+                    }
+                }
+                fetch(codes, scales, e);
+            }
+        }
+    }
+    // eight columns of every lane at a time: 32 sums (four parts of eight waves) of 128 columns
+    constexpr int kPass = 8, kPitch = 16 * kPass + 1;
+    float* red = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int n0 = 0; n0 < CW; n0 += kPass) {
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kPass; ++n) red[(wave * 4 + lk) * kPitch + li * kPass + n] = acc[n0 + n];
+        __syncthreads();
+        // four threads share a column
+        const int p = tid >> 2, h = tid & 3;
+        float v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v += red[(k * 4 + h) * kPitch + p];
+        v += __shfl_xor(v, 1, 64);
+        v += __shfl_xor(v, 2, 64);
+        const int64_t at = j0 + p / kPass * CW + n0 + p % kPass;
+        if (h == 0 && at < a.r) {
+            if (part)
+                part[split * a.r + at] = v;
+            else
+                mx_store(a, 0, at, v);
         }
     }
 }
@@ -545,7 +662,7 @@ hipError_t launch_few_cols(const MxArgs& a, hipStream_t st) {
 constexpr int kTBytes = 16;
 int64_t t_groups(const MxArgs& a) { return ceil_div(a.r, 16 * kTBytes * 8 / a.A.bits); }
 int64_t t_rows(const MxArgs& a) {
-    const int64_t splits = std::max<int64_t>(1, 512 / t_groups(a));
+    const int64_t splits = std::max<int64_t>(1, (a.s == 1 ? 1024 : 512) / t_groups(a));
     const int64_t unit = 32 * kWaves;
     return std::max<int64_t>(2, ceil_div(ceil_div(a.q, splits), unit)) * unit;
 }
@@ -560,6 +677,13 @@ hipError_t launch_few_t(const MxArgs& a, hipStream_t st) {
     constexpr int kPitch = 16 * 4 + 1;
     const int64_t lds = std::max<int64_t>(staged * cols * 2, kWaves * cols * kPitch * 4);
     float* part = splits > 1 ? static_cast<float*>(a.workspace) : nullptr;
+    if (a.s == 1) {
+        const int64_t rows = std::min<int64_t>(per, 8192);
+        const int64_t bytes = std::max<int64_t>(rows * 4, 32 * (16 * 8 + 1) * 4);
+        mx_vector_t_kernel<BITS><<<dim3(static_cast<uint32_t>(groups * splits)), kThreads, bytes, st>>>(a, per, static_cast<int>(rows), groups, part);
+        const hipError_t e = hipGetLastError();
+        return e != hipSuccess || !part ? e : launch_mx_join(a, part, splits, a.r, st);
+    }
     mx_few_t_kernel<BITS, kTBytes><<<dim3(static_cast<uint32_t>(groups * splits)), kThreads, lds, st>>>(
         a, planes, per, static_cast<int>(staged), groups, part);
     hipError_t e = hipGetLastError();
