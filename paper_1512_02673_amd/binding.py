@@ -8,6 +8,7 @@ library has not been built.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import re
 
@@ -533,25 +534,35 @@ class MXMatrix:
     """A microscaled matrix of `cols` columns: codes (uint8, rows x code pitch) and scales (uint8,
     rows x scale pitch) in the layout of include/coded.h.  rows(a, b) is a run of its rows."""
 
-    __slots__ = ("codes", "scales", "cols", "fmt", "ldc", "lds")
+    __slots__ = ("codes", "scales", "rows_", "cols", "fmt", "ldc", "lds")
 
     def __init__(self, codes, scales, cols: int, fmt: int):
-        if fmt != CODED_MX4 and fmt != CODED_MX8:
+        if fmt == CODED_MX4:
+            need_c = (cols + 31) // 32 * 16
+        elif fmt == CODED_MX8:
+            need_c = (cols + 31) // 32 * 32
+        else:
             raise ValueError("the format must be CODED_MX4 or CODED_MX8")
-        need_c, need_s = -(-cols // 32) * (16 if fmt == CODED_MX4 else 32), -(-cols // 128) * 4
-        uint8, n = _torch().uint8, codes.shape[0]
-        if codes.dtype != uint8 or codes.dim() != 2 or codes.shape[1] < need_c or (need_c and codes.stride(1) != 1):
-            raise ValueError(f"codes must be uint8, rows of at least {need_c} bytes")
-        if scales.dtype != uint8 or scales.dim() != 2 or scales.shape[1] < need_s or (need_s and scales.stride(1) != 1):
-            raise ValueError(f"scales must be uint8, rows of at least {need_s} bytes")
-        if scales.shape[0] != n:
+        need_s = (cols + 127) // 128 * 4
+        uint8 = _torch().uint8
+        if codes.dtype is not uint8 or scales.dtype is not uint8 or codes.dim() != 2 or scales.dim() != 2:
+            raise ValueError("codes and scales must be uint8, rows of bytes")
+        n, width = codes.shape
+        n_s, width_s = scales.shape
+        ldc, step = codes.stride()
+        lds, step_s = scales.stride()
+        if width < need_c or (need_c and step != 1):
+            raise ValueError(f"codes must be rows of at least {need_c} bytes")
+        if width_s < need_s or (need_s and step_s != 1):
+            raise ValueError(f"scales must be rows of at least {need_s} bytes")
+        if n != n_s:
             raise ValueError("codes and scales must have the same number of rows")
-        self.codes, self.scales, self.cols, self.fmt = codes, scales, cols, fmt
-        self.ldc, self.lds = (codes.stride(0), scales.stride(0)) if n > 1 and cols > 0 else (need_c, need_s)
+        self.codes, self.scales, self.rows_, self.cols, self.fmt = codes, scales, n, cols, fmt
+        self.ldc, self.lds = (ldc, lds) if n > 1 and cols > 0 else (need_c, need_s)
 
     @property
     def shape(self):
-        return self.codes.shape[0], self.cols
+        return self.rows_, self.cols
 
     def rows(self, begin: int, end: int) -> "MXMatrix":
         return MXMatrix(self.codes[begin:end], self.scales[begin:end], self.cols, self.fmt)
@@ -579,6 +590,7 @@ def _mx_dense(t, name):
     return rows, cols, ld if rows > 1 else max(cols, 1), dt
 
 
+@functools.lru_cache(maxsize=256)
 def coded_mx_sizes(fmt: int, r: int):
     """(code pitch, scale pitch) in bytes of rows of r columns."""
     c, s = ctypes.c_int64(), ctypes.c_int64()
@@ -590,8 +602,8 @@ def alloc_mx(q: int, r: int, fmt: int, device="cuda") -> MXMatrix:
     """Room for a q x r microscaled matrix (not cleared: coded_mx_quantize writes all that is read)."""
     torch = _torch()
     c, s = coded_mx_sizes(fmt, r)
-    return MXMatrix(torch.empty((q, c), dtype=torch.uint8, device=device),
-                    torch.empty((q, s), dtype=torch.uint8, device=device), r, fmt)
+    empty, uint8 = torch.empty, torch.uint8
+    return MXMatrix(empty((q, c), dtype=uint8, device=device), empty((q, s), dtype=uint8, device=device), r, fmt)
 
 
 def coded_mx_quantize(A, M: MXMatrix, stream=None) -> None:
@@ -610,6 +622,7 @@ def coded_mx_dequantize(M: MXMatrix, out, stream=None) -> None:
     _check(lib().coded_mx_dequantize(*M._args(), q, r, dt, out.data_ptr(), ldo, _stream(stream)))
 
 
+@functools.lru_cache(maxsize=256)
 def coded_mx_workspace(transposed: bool, fmt: int, q: int, r: int, x_dt: int, s: int, x_rows: bool = False,
                        y_rows: bool = False) -> int:
     """Bytes of workspace of coded_mx_mm, or of coded_mx_mm_t when transposed."""

@@ -140,7 +140,7 @@ __global__ __launch_bounds__(256) void mx_order_kernel(MxArgs a, int planes, int
     for (int h = 0; h < planes; ++h) at[h * a.s] = h == 0 ? v[0] : h == 1 ? v[1] : v[2];
 }
 
-template <int BITS, int NT, int RT, int COLS, int CP>
+template <int BITS, int NT, int RT, int COLS, int CP, bool NTL>
 __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArgs a, int wk_log_, int planes, const u32x4_t* image) {
     constexpr int kStep = kStepOf<BITS>;
     constexpr int U = 16 / BITS;                   // operands of a piece
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
         for (int t = 0; t < 4; ++t) {
             const bool in = p0 + 4 * t < static_cast<int>(pieces_a);
 #pragma unroll
-            for (int x = 0; x < RT; ++x) w[d][x][t] = codes.four(in ? code_row[x] + (p0 + 4 * t) * 16 : kNowhere);
+            for (int x = 0; x < RT; ++x) w[d][x][t] = codes.four<NTL>(in ? code_row[x] + (p0 + 4 * t) * 16 : kNowhere);
         }
 #pragma unroll
         for (int x = 0; x < RT; ++x) {
@@ -327,8 +327,8 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
 
 // ---------------------------------------------------------------- across the blocks
 
-// Z = A^T U.  A wave takes W bytes of 16 neighbouring lanes' columns and walks
-// down the rows, 32 a step: lane (li, lk) loads W bytes of rows 8 lk .. 8 lk +
+// Z = A^T U.  A wave takes 16 bytes of 16 neighbouring lanes' columns and walks
+// down the rows, 32 a step: lane (li, lk) loads 16 bytes of rows 8 lk .. 8 lk +
 // 7, which is an 8 x CW piece of A with all the terms that the matrix operand
 // of each of its CW columns needs of this lane: result tile n is column n of
 // every lane's piece.  The conversion makes pairs along a row and the operand
@@ -342,10 +342,10 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
 //
 // Rows past q repeat the last one and meet zeros of U; columns past r repeat
 // the last block and are not stored.
-template <int BITS, int W>
-__global__ __launch_bounds__(kThreads, W == 16 ? 2 : 4) void mx_few_t_kernel(MxArgs a, int planes, int64_t per, int rows_staged, int64_t groups,
+template <int BITS, bool NTL>
+__global__ __launch_bounds__(kThreads, 2) void mx_few_t_kernel(MxArgs a, int planes, int64_t per, int rows_staged, int64_t groups,
                                                                float* part) {
-    constexpr int CW = W * 8 / BITS;   // columns of a lane
+    constexpr int CW = 128 / BITS;     // columns of a lane
     constexpr int kCols = 16 * CW;     // and of a workgroup
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
@@ -358,22 +358,18 @@ __global__ __launch_bounds__(kThreads, W == 16 ? 2 : 4) void mx_few_t_kernel(MxA
     const int64_t t0 = split * per, t1 = lesser(t0 + per, a.q);
     const int s = static_cast<int>(a.s), cols = planes * s;
     const int64_t j0 = group * kCols;
-    typedef unsigned int words_t __attribute__((ext_vector_type(W / 4)));
-    words_t w[8];
+    u32x4_t w[8];
     uint32_t sc[8];
     // rows past q read as zeros; columns past r are other bytes of A, or zeros, and are not stored
     const int64_t blocks = ceil_div(a.r, kMxBlock), c0_ = j0 * BITS / 8, b0_ = j0 / kMxBlock;
-    const uint32_t code_at = static_cast<uint32_t>(8 * lk * a.A.ldc) + li * W, scale_at = static_cast<uint32_t>(8 * lk * a.A.lds) + li * CW / kMxBlock;
+    const uint32_t code_at = static_cast<uint32_t>(8 * lk * a.A.ldc) + li * 16, scale_at = static_cast<uint32_t>(8 * lk * a.A.lds) + li * CW / kMxBlock;
     const auto fetch = [&](int64_t t) {
         const int64_t have = lesser(a.q - t, 32) - 1;
         const Window codes(a.A.codes + t * a.A.ldc + c0_, have < 0 ? 0 : have * a.A.ldc + blocks * 4 * BITS - c0_);
         const Window scales(a.A.scales + t * a.A.lds + b0_, have < 0 ? 0 : have * a.A.lds + blocks - b0_);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if constexpr (W == 16)
-                w[e] = codes.four(code_at + static_cast<uint32_t>(e * a.A.ldc));
-            else
-                w[e] = codes.two(code_at + static_cast<uint32_t>(e * a.A.ldc));
+            w[e] = codes.four<NTL>(code_at + static_cast<uint32_t>(e * a.A.ldc));
             sc[e] = scales.byte(scale_at + static_cast<uint32_t>(e * a.A.lds));
         }
     };
@@ -395,7 +391,7 @@ __global__ __launch_bounds__(kThreads, W == 16 ? 2 : 4) void mx_few_t_kernel(MxA
         __syncthreads();
         for (; mine < end; mine += 32 * kWaves) {
             const bf16x8 u = *reinterpret_cast<const bf16x8*>(smem + static_cast<int>(mine - c0) / 8 * cols * 16 + col);
-            words_t cw[8];
+            u32x4_t cw[8];
             float scale[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -419,7 +415,7 @@ __global__ __launch_bounds__(kThreads, W == 16 ? 2 : 4) void mx_few_t_kernel(MxA
                 acc[n + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(u, __builtin_bit_cast(bf16x8, odd), acc[n + 1], 0, 0, 0);
             };
 #pragma unroll
-            for (int word = 0; word < W / 4; ++word) {
+            for (int word = 0; word < 4; ++word) {
                 pair(std::integral_constant<int, 0>{}, word);
                 pair(std::integral_constant<int, 1>{}, word);
                 if constexpr (BITS == 4) {
@@ -465,7 +461,7 @@ __global__ __launch_bounds__(kThreads, W == 16 ? 2 : 4) void mx_few_t_kernel(MxA
 // the same registers take the row 256 further down at once, and with 32 sums
 // instead of 128 twice as many waves have loads under way.  The sums of the four
 // parts of a wave, of the eight waves and of the workgroups are added at the end.
-template <int BITS>
+template <int BITS, bool NTL>
 __global__ __launch_bounds__(kThreads, 4) void mx_vector_t_kernel(MxArgs a, int64_t per, int rows_staged, int64_t groups, float* part) {
     constexpr int CW = 128 / BITS, kCols = 16 * CW;   // columns of a lane, and of a workgroup
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -489,7 +485,7 @@ __global__ __launch_bounds__(kThreads, 4) void mx_vector_t_kernel(MxArgs a, int6
         return Window(a.A.scales + t * a.A.lds + b0_, have < 0 ? 0 : have * a.A.lds + blocks - b0_);
     };
     const auto fetch = [&](const Window& codes, const Window& scales, int e) {
-        w[e] = codes.four(code_at + static_cast<uint32_t>(e * a.A.ldc));
+        w[e] = codes.four<NTL>(code_at + static_cast<uint32_t>(e * a.A.ldc));
         sc[e] = scales.byte(scale_at + static_cast<uint32_t>(e * a.A.lds));
     };
     float acc[CW] = {};
@@ -583,6 +579,9 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxArgs a, const float* par
     }
 }
 
+// Codes that do not stay in the memory-side cache from call to call.
+bool streamed(const MxArgs& a) { return streams(a.q * ceil_div(a.r, kMxBlock) * 4 * a.A.bits); }
+
 int planes_of(const MxArgs& a) { return a.x_bits || a.x_bf16 ? 1 : 3; }
 
 // How a product along the blocks is cut up.
@@ -630,7 +629,8 @@ hipError_t launch_few(const MxArgs& a, const FewPlan& p, hipStream_t st) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    mx_few_kernel<BITS, NT, RT, COLS, CP><<<dim3(static_cast<uint32_t>(blocks)), kThreads, p.lds, st>>>(a, p.wk_log, planes, image);
+    const auto kernel = streamed(a) ? mx_few_kernel<BITS, NT, RT, COLS, CP, true> : mx_few_kernel<BITS, NT, RT, COLS, CP, false>;
+    kernel<<<dim3(static_cast<uint32_t>(blocks)), kThreads, p.lds, st>>>(a, p.wk_log, planes, image);
     return hipGetLastError();
     }
 }
@@ -659,8 +659,7 @@ hipError_t launch_few_cols(const MxArgs& a, hipStream_t st) {
 
 // Workgroups that share the columns of mx_few_t_kernel: about 512 in all, each
 // with at least two steps for each of its waves.
-constexpr int kTBytes = 16;
-int64_t t_groups(const MxArgs& a) { return ceil_div(a.r, 16 * kTBytes * 8 / a.A.bits); }
+int64_t t_groups(const MxArgs& a) { return ceil_div(a.r, 16 * 128 / a.A.bits); }
 int64_t t_rows(const MxArgs& a) {
     const int64_t splits = std::max<int64_t>(1, (a.s == 1 ? 1024 : 512) / t_groups(a));
     const int64_t unit = 32 * kWaves;
@@ -680,11 +679,13 @@ hipError_t launch_few_t(const MxArgs& a, hipStream_t st) {
     if (a.s == 1) {
         const int64_t rows = std::min<int64_t>(per, 8192);
         const int64_t bytes = std::max<int64_t>(rows * 4, 32 * (16 * 8 + 1) * 4);
-        mx_vector_t_kernel<BITS><<<dim3(static_cast<uint32_t>(groups * splits)), kThreads, bytes, st>>>(a, per, static_cast<int>(rows), groups, part);
+        const auto vector = streamed(a) ? mx_vector_t_kernel<BITS, true> : mx_vector_t_kernel<BITS, false>;
+        vector<<<dim3(static_cast<uint32_t>(groups * splits)), kThreads, bytes, st>>>(a, per, static_cast<int>(rows), groups, part);
         const hipError_t e = hipGetLastError();
         return e != hipSuccess || !part ? e : launch_mx_join(a, part, splits, a.r, st);
     }
-    mx_few_t_kernel<BITS, kTBytes><<<dim3(static_cast<uint32_t>(groups * splits)), kThreads, lds, st>>>(
+    const auto kernel = streamed(a) ? mx_few_t_kernel<BITS, true> : mx_few_t_kernel<BITS, false>;
+    kernel<<<dim3(static_cast<uint32_t>(groups * splits)), kThreads, lds, st>>>(
         a, planes, per, static_cast<int>(staged), groups, part);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !part) return e;

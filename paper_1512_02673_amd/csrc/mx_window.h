@@ -22,7 +22,9 @@ struct Window {
     __device__ __forceinline__ Window(const void* base, int64_t bytes)
         : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, static_cast<int>(bytes < 0 ? 0 : lesser(bytes, 0xFFFFFFFF)),
                                                  0x00027000)) {}
-    __device__ __forceinline__ u32x4_t four(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0); }
+    // NTL: non-temporal, for what does not stay in the memory-side cache until it is read again
+    template <bool NTL = false>
+    __device__ __forceinline__ u32x4_t four(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, NTL ? 2 : 0); }
     __device__ __forceinline__ u32x2_t two(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b64(rsrc, at, 0, 0); }
     __device__ __forceinline__ uint32_t word(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0); }
     __device__ __forceinline__ uint32_t two_bytes(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0); }
