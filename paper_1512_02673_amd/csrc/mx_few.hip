@@ -167,28 +167,33 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
         code_row[x] = row * static_cast<uint32_t>(a.A.ldc);
         scale_row[x] = row * static_cast<uint32_t>(a.A.lds);
     }
-    // Codes of the next steps are on their way: of two where the registers allow it, else of one.
-    constexpr int D = NT == 1 ? 2 : 1;
+    // Codes of the next two steps are on their way: each piece's registers take the piece two steps on as soon as
+    // it is used up.
+    constexpr int D = 2;
     u32x4_t w[D][RT][4];
     typedef unsigned int scales_t __attribute__((ext_vector_type(kScales)));
     scales_t sc[D][RT];
-    const auto fetch = [&](int step, auto S) {
-        constexpr int d = S.value % D;
-        const int p0 = step * 16 + lk, b0 = step * kScales * 4;
+    const auto fetch_piece = [&](int step, int t, auto S) {
+        const int p = step * 16 + 4 * t + lk;
+        const bool in = p < static_cast<int>(pieces_a);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const bool in = p0 + 4 * t < static_cast<int>(pieces_a);
-#pragma unroll
-            for (int x = 0; x < RT; ++x) w[d][x][t] = codes.four<NTL>(in ? code_row[x] + (p0 + 4 * t) * 16 : kNowhere);
-        }
+        for (int x = 0; x < RT; ++x) w[S.value][x][t] = codes.four<NTL>(in ? code_row[x] + p * 16 : kNowhere);
+    };
+    const auto fetch_scales = [&](int step, auto S) {
+        const uint32_t b0 = step * kScales * 4;
 #pragma unroll
         for (int x = 0; x < RT; ++x) {
-            const uint32_t at = p0 < static_cast<int>(pieces_a) + lk ? scale_row[x] + b0 : kNowhere;   // the step's first piece is in the row
+            const uint32_t at = step * 16 < static_cast<int>(pieces_a) ? scale_row[x] + b0 : kNowhere;   // the step's first piece is in the row
             if constexpr (BITS == 4)
-                sc[d][x] = scales.four(at);
+                sc[S.value][x] = scales.four(at);
             else
-                sc[d][x] = scales.two(at);
+                sc[S.value][x] = scales.two(at);
         }
+    };
+    const auto fetch = [&](int step, auto S) {
+        fetch_scales(step, S);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) fetch_piece(step, t, S);
     };
 
     int col[NT];   // byte offset of this lane's column of a column tile
@@ -197,10 +202,9 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
     const int step_bytes = kStep * pitch * 2;
 
     f32x4_t sum[RT][NT] = {};
-    // a step's sums from X at xs; the codes of the step `next` are on their way before they begin
+    // a step's sums from X at xs; `next` is the step two rounds on
     const auto compute = [&](const char* xs, int step, int next, auto S) {
-        constexpr int d = S.value % D;
-        u32x4_t cw[RT][4];
+        constexpr int d = S.value;
         float scale[RT][4];
         const int left = static_cast<int>(blocks) - step * kScales * 4;
         if (left < 4 * kScales) {   // the row's last step
@@ -213,12 +217,11 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
         for (int x = 0; x < RT; ++x)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                cw[x][t] = w[d][x][t];
                 // piece 4 t + lk: byte lk of word t, or (two pieces a block) byte 2 t + lk / 2
                 const uint32_t byte = BITS == 4 ? sc[d][x][t] >> (8 * lk) : sc[d][x][t / 2] >> (16 * (t & 1) + 8 * (lk >> 1));
                 scale[x][t] = mx_scale(byte & 0xFFu);
             }
-        fetch(next, S);
+        fetch_scales(next, S);
         f32x4_t acc[RT][NT] = {};
         // X's operands are read one part ahead
         bf16x8 xv[2][NT];
@@ -231,11 +234,12 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
             if constexpr (p + 1 < 4 * U) read(p + 1);
 #pragma unroll
             for (int x = 0; x < RT; ++x) {
-                const bf16x8 av = operand<BITS, p % U>(cw[x][p / U], scale[x][p / U]);
+                const bf16x8 av = operand<BITS, p % U>(w[d][x][p / U], scale[x][p / U]);
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
                     acc[x][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, xv[p & 1][n], acc[x][n], 0, 0, 0);
             }
+            if constexpr (p % U == U - 1) fetch_piece(next, p / U, S);
             if constexpr (NT > 1) __builtin_amdgcn_sched_barrier(0);
         };
         read(0);
@@ -255,7 +259,7 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
     typedef std::integral_constant<int, 0> even;
     typedef std::integral_constant<int, 1> odd;
     fetch(step_at(0), even{});
-    if constexpr (D == 2) fetch(step_at(1), odd{});
+    fetch(step_at(1), odd{});
     if constexpr (COLS) {
         const int round = WK * step_bytes;
         const Window x(image, steps * step_bytes);
