@@ -251,9 +251,10 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
     };
 
     // Rounds of one step of each of the WK waves.  Workgroups start at different ones: in step, they would all
-    // read the same columns of their rows, a whole row apart.
+    // read the same columns of their rows, a whole row apart (65536 x 8192, one vector: 64 us, so 54; with every
+    // workgroup at another 59.  131072 x 16384, 64 columns: 368 and 355, with every workgroup at another 327).
     const int rounds = static_cast<int>(ceil_div(steps, WK)), none = static_cast<int>(steps) + WK;
-    const int first = blockIdx.x % rounds;
+    const int first = NT > 1 ? blockIdx.x % rounds : ((blockIdx.x % 8) * 2 + (blockIdx.x / 8 & 1)) * rounds / 16;
     const auto round_at = [&](int i) { return first + i < rounds ? first + i : first + i - rounds; };   // i <= rounds
     const auto step_at = [&](int i) { return i < rounds ? round_at(i) * WK + wk : none; };
     typedef std::integral_constant<int, 0> even;
