@@ -445,3 +445,77 @@ def test_workspace_too_small_is_refused(lib, torch):
                           workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
     assert e.value.status == lib.CODED_ERR_ARG
     assert math.isfinite(need)
+
+
+def whole_codes(torch, rows, cols, g):
+    """Codes of whole numbers up to 6 (4 bits) with scales of 1, made on the GPU, and the fp64 values."""
+    table = torch.tensor([0, 2, 4, 5, 6, 7, 10, 12, 13, 14, 15], device="cuda", dtype=torch.uint8)
+    pick = torch.randint(0, len(table), (rows, -(-cols // 32) * 32), device="cuda", generator=g)
+    codes = table[pick]
+    codes[:, cols:] = 0
+    value = torch.tensor(om.format_values(4), device="cuda")
+    v = value[codes.int()][:, :cols]
+    packed = codes[:, 0::2] | (codes[:, 1::2] << 4)
+    return packed.contiguous(), torch.full((rows, -(-cols // 128) * 4), 127, dtype=torch.uint8, device="cuda"), v
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("x", ["f32", "bf16", "mx4"])
+@pytest.mark.parametrize("n,k,s", [(8192, 16500, 2048), (8448, 200, 2100), (520, 66000, 260)])
+def test_whole_numbers_are_exact_over_rounds_of_tiles(lib, torch, transposed, x, n, k, s):
+    """More than a round of large tiles with some left over, sums of more than one fp32 chain, and sums split many times."""
+    if transposed and x == "mx4":
+        pytest.skip("U is dense")
+    g = torch.Generator(device="cuda").manual_seed(n + k + s)
+    q, r = (k, n) if transposed else (n, k)
+    codes, scales, A = whole_codes(torch, q, r, g)
+    M = lib.MXMatrix(codes, scales, r, lib.CODED_MX4)
+    A = A.t() if transposed else A
+    for order in (0, 3):
+        if x == "mx4":
+            xc, xs, X64 = whole_codes(torch, s, k, g)
+            X, X64 = lib.MXMatrix(xc, xs, k, lib.CODED_MX4), X64.t()
+        else:
+            X = torch.randint(-7, 8, (s, k) if order & 1 else (k, s), device="cuda", generator=g).to(torch.float32 if x == "f32" else torch.bfloat16)
+            X64 = X.double().t() if order & 1 else X.double()
+        Y = torch.empty((s, n) if order & 2 else (n, s), device="cuda")
+        (lib.coded_mx_mm_t if transposed else lib.coded_mx_mm)(M, X, Y, x_rows=bool(order & 1) or x == "mx4", y_rows=bool(order & 2))
+        want = A @ X64
+        assert float(want.abs().max()) < 2 ** 24
+        assert torch.equal(Y.double(), want.t() if order & 2 else want)
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+def test_x_by_columns_at_any_address(lib, torch, transposed):
+    """Columns of bf16 at even and odd row strides and addresses: read as they are, or copied."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for n, k, s in ((700, 300, 130), (8200, 130, 1100)):
+        q, r = (k, n) if transposed else (n, k)
+        codes, scales, A = whole_codes(torch, q, r, g)
+        M = lib.MXMatrix(codes, scales, r, lib.CODED_MX4)
+        A = A.t() if transposed else A
+        for ld, off in ((s, 0), (s + 1, 0), (s + 2, 1), (s + 2, 2), (s + 7, 3)):
+            flat = torch.full((k * ld + off + 8,), float("nan"), dtype=torch.bfloat16, device="cuda")
+            X = flat[off:off + k * ld].view(k, ld)[:, :s]
+            X.copy_(torch.randint(-7, 8, (k, s), device="cuda", generator=g))
+            Y = torch.empty((n, s), device="cuda")
+            (lib.coded_mx_mm_t if transposed else lib.coded_mx_mm)(M, X, Y)
+            assert torch.equal(Y.double(), A @ X.double()), (ld, off)
+
+
+def test_rows_of_more_than_eight_megabytes(lib, torch):
+    """Offsets within a tile's rows that pass 32 bits take the general kernel."""
+    r = (1 << 24) + 5
+    g = torch.Generator(device="cuda").manual_seed(4)
+    codes, scales, A = whole_codes(torch, 2, r, g)
+    codes[:, 1 << 18:] = 0          # sums below 2^24
+    A[:, 1 << 19:] = 0
+    M = lib.MXMatrix(codes, scales, r, lib.CODED_MX4)
+    X = torch.randint(-7, 8, (r, 2), device="cuda", generator=g).to(torch.bfloat16)
+    Y = torch.empty((2, 2), device="cuda")
+    lib.coded_mx_mm(M, X, Y)
+    assert torch.equal(Y.double(), A @ X.double())
+    U = torch.tensor([[1.0, 2.0], [3.0, -1.0]], device="cuda")
+    Z = torch.empty((r, 2), device="cuda")
+    lib.coded_mx_mm_t(M, U, Z)
+    assert torch.equal(Z.double(), A.t() @ U.double())
