@@ -677,6 +677,8 @@ def _mx_product(transposed, M, X, Y, x_rows, y_rows, alpha, beta, C, workspace, 
         if wsb:
             workspace = _torch().empty(wsb, dtype=_torch().uint8, device=Y.device)
             wsp = workspace.data_ptr()
+            if stream is not None:   # its memory is not handed out again before that stream is done with it
+                workspace.record_stream(stream)
     elif workspace is not None:
         wsp, wsb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     order = bool(x_rows) | bool(y_rows) << 1

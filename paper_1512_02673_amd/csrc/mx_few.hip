@@ -141,7 +141,8 @@ __global__ __launch_bounds__(256) void mx_order_kernel(MxArgs a, int planes, int
 }
 
 template <int BITS, int NT, int RT, int COLS, int CP, bool NTL>
-__global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArgs a, int wk_log_, int planes, const u32x4_t* image) {
+__global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArgs a, int wk_log_, int planes, const u32x4_t* image, int64_t groups,
+                                                                          int rounds_a_split, float* part) {
     constexpr int kStep = kStepOf<BITS>;
     constexpr int U = 16 / BITS;                   // operands of a piece
     constexpr int kScales = BITS == 4 ? 4 : 2;     // words of scales of a step
@@ -154,7 +155,8 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
     const int wk = wave & (WK - 1), wr = wave / WK;
     const int s = static_cast<int>(a.s), cols = planes * s, pitch = COLS ? COLS : cols;   // pitch: columns that X is laid out in
     const int rows = kWaves / WK * 16 * RT;
-    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * rows;
+    const int64_t group = blockIdx.x % groups, split = blockIdx.x / groups;
+    const int64_t row0 = group * rows;
     const int64_t blocks = ceil_div(a.r, kMxBlock), pieces_a = blocks * BITS / 4, steps = ceil_div(a.r, kStep);
 
     const int64_t have = lesser(a.q - row0, rows) - 1;
@@ -253,9 +255,10 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
     // Rounds of one step of each of the WK waves.  Workgroups start at different ones: in step, they would all
     // read the same columns of their rows, a whole row apart (65536 x 8192, one vector: 64 us, so 54; with every
     // workgroup at another 59.  131072 x 16384, 64 columns: 368 and 355, with every workgroup at another 327).
-    const int rounds = static_cast<int>(ceil_div(steps, WK)), none = static_cast<int>(steps) + WK;
+    const int begin = static_cast<int>(split) * rounds_a_split;
+    const int rounds = static_cast<int>(lesser(rounds_a_split, ceil_div(steps, WK) - begin)), none = static_cast<int>(steps) + WK;
     const int first = NT > 1 ? blockIdx.x % rounds : ((blockIdx.x % 8) * 2 + (blockIdx.x / 8 & 1)) * rounds / 16;
-    const auto round_at = [&](int i) { return first + i < rounds ? first + i : first + i - rounds; };   // i <= rounds
+    const auto round_at = [&](int i) { return begin + (first + i < rounds ? first + i : first + i - rounds); };   // i <= rounds
     const auto step_at = [&](int i) { return i < rounds ? round_at(i) * WK + wk : none; };
     typedef std::integral_constant<int, 0> even;
     typedef std::integral_constant<int, 1> odd;
@@ -273,7 +276,7 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
 #pragma unroll
             for (int i = 0; i < CP; ++i) *reinterpret_cast<u32x4_t*>(to + (tid + i * kThreads) * 16) = xr[i];
         };
-        copy_in(first);
+        copy_in(round_at(0));
         copy_out(smem);
         const auto turn = [&](int i, auto S) {
             __syncthreads();
@@ -326,7 +329,10 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
         float v = 0.0f;
         for (int h = 0; h < planes; ++h)
             for (int k = 0; k < WK; ++k) v += red[(k * rows + t) * kPitch + h * s + c];
-        mx_store(a, c, row0 + t, v);
+        if (part)
+            part[(split * s + c) * a.q + row0 + t] = v;
+        else
+            mx_store(a, c, row0 + t, v);
     }
 }
 
@@ -574,6 +580,7 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxArgs a, const float* par
     const int g = threadIdx.x >> 5;
     float v = 0.0f;
     if (at < n)
+#pragma unroll 4
         for (int64_t p = g; p < splits; p += 8) v += part[(p * a.s + side) * n + at];
     red[g][threadIdx.x & 31] = v;
     __syncthreads();
@@ -587,6 +594,32 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxArgs a, const float* par
 // Codes that do not stay in the memory-side cache from call to call.
 bool streamed(const MxArgs& a) { return streams(a.q * ceil_div(a.r, kMxBlock) * 4 * a.A.bits); }
 
+// The same for many sides, 32 of them and 32 results a workgroup: read along the results and, where a row of Y
+// holds the sides, turned in shared memory, so that it is written along them.
+__global__ __launch_bounds__(256) void mx_join_tile_kernel(MxArgs a, const float* part, int64_t splits, int64_t n) {
+    __shared__ float tile[32][33];
+    const int64_t tiles = ceil_div(n, 32), j0 = blockIdx.x % tiles * 32, i0 = blockIdx.x / tiles * 32;
+    const int lo = threadIdx.x & 31, hi = threadIdx.x >> 5;
+    float v[4] = {};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (i0 + hi + 8 * e < a.s && j0 + lo < n)
+#pragma unroll 4
+            for (int64_t p = 0; p < splits; ++p) v[e] += part[(p * a.s + i0 + hi + 8 * e) * n + j0 + lo];
+    if (a.y_rows) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i0 + hi + 8 * e < a.s && j0 + lo < n) mx_store(a, i0 + hi + 8 * e, j0 + lo, v[e]);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tile[hi + 8 * e][lo] = v[e];
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (i0 + lo < a.s && j0 + hi + 8 * e < n) mx_store(a, i0 + lo, j0 + hi + 8 * e, tile[lo][hi + 8 * e]);
+}
+
 int planes_of(const MxArgs& a) { return a.x_bits || a.x_bf16 ? 1 : 3; }
 
 // How a product along the blocks is cut up.
@@ -594,6 +627,8 @@ struct FewPlan {
     int cols;            // that X is laid out in in the workspace; 0: it is not
     int rt, wk_log;      // row tiles of a wave, log2 of the waves on the same rows
     int64_t steps, lds, image_bytes;
+    int64_t groups, splits, per;   // workgroups over the rows, and over the terms with `per` rounds each
+    int64_t part_bytes;
 };
 FewPlan few_plan(const MxArgs& a) {
     FewPlan p{};
@@ -615,6 +650,18 @@ FewPlan few_plan(const MxArgs& a) {
         ++p.wk_log;
     const int64_t red = kWaves * 16 * p.rt * 16 * (cols <= 16 ? 1 : p.cols / 16) * 4;
     p.lds = std::max(red, p.cols ? 2 * (step * p.cols * 2 << p.wk_log) : x_bytes);
+    // A round takes 0.9, 1.7 or 3.6 us with up to one workgroup a compute unit (X's 16, 32 or 64 columns).  Where
+    // few rows leave units idle they share the rounds, if that saves more than adding the parts up takes
+    // (16384 x 16384, 64 columns: 128 us, with four workgroups on the same rows 60).
+    const int64_t rounds = ceil_div(p.steps, int64_t(1) << p.wk_log);
+    p.groups = ceil_div(a.q, (kWaves >> p.wk_log) * 16 * p.rt);
+    p.splits = p.cols ? std::max<int64_t>(1, std::min(256 / p.groups, rounds / 2)) : 1;
+    const double us = rounds * (p.cols <= 16 ? 0.9 : p.cols == 32 ? 1.7 : 3.6);
+    if (us - us / p.splits < 8 + p.splits * a.s * a.q * 4 / 2e6) p.splits = 1;
+    p.per = std::max<int64_t>(1, ceil_div(rounds, p.splits));
+    p.splits = std::max<int64_t>(1, ceil_div(rounds, p.per));
+    p.image_bytes = (p.image_bytes + 255) / 256 * 256;
+    p.part_bytes = p.splits > 1 ? p.splits * a.s * a.q * 4 : 0;
     return p;
 }
 
@@ -623,20 +670,22 @@ hipError_t launch_few(const MxArgs& a, const FewPlan& p, hipStream_t st) {
     if constexpr (CP * kThreads < kStepOf<BITS> / 8 * COLS) {   // less than a step of X a round
         return hipErrorInvalidConfiguration;
     } else {
-    const int planes = planes_of(a);
-    const int64_t blocks = ceil_div(a.q, (kWaves >> p.wk_log) * 16 * RT);
-    if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
-    u32x4_t* image = static_cast<u32x4_t*>(a.workspace);
-    if constexpr (COLS) {
-        const int64_t pieces = p.steps * (kStepOf<BITS> / 8), groups = ceil_div(pieces * a.s, 256);
-        if (!grid_fits(groups, 256)) return hipErrorInvalidConfiguration;
-        mx_order_kernel<BITS><<<dim3(static_cast<uint32_t>(groups)), 256, 0, st>>>(a, planes, pieces, COLS, image);
+        const int planes = planes_of(a);
+        const int64_t blocks = p.groups * p.splits;
+        if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
+        u32x4_t* image = static_cast<u32x4_t*>(a.workspace);
+        float* part = p.splits > 1 ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + p.image_bytes) : nullptr;
+        if constexpr (COLS) {
+            const int64_t pieces = p.steps * (kStepOf<BITS> / 8), threads = ceil_div(pieces * a.s, 256);
+            if (!grid_fits(threads, 256)) return hipErrorInvalidConfiguration;
+            mx_order_kernel<BITS><<<dim3(static_cast<uint32_t>(threads)), 256, 0, st>>>(a, planes, pieces, COLS, image);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        const auto kernel = streamed(a) ? mx_few_kernel<BITS, NT, RT, COLS, CP, true> : mx_few_kernel<BITS, NT, RT, COLS, CP, false>;
+        kernel<<<dim3(static_cast<uint32_t>(blocks)), kThreads, p.lds, st>>>(a, p.wk_log, planes, image, p.groups, static_cast<int>(p.per), part);
         const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    const auto kernel = streamed(a) ? mx_few_kernel<BITS, NT, RT, COLS, CP, true> : mx_few_kernel<BITS, NT, RT, COLS, CP, false>;
-    kernel<<<dim3(static_cast<uint32_t>(blocks)), kThreads, p.lds, st>>>(a, p.wk_log, planes, image);
-    return hipGetLastError();
+        return e != hipSuccess || !part ? e : launch_mx_join(a, part, p.splits, a.q, st);
     }
 }
 
@@ -700,6 +749,13 @@ hipError_t launch_few_t(const MxArgs& a, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_mx_join(const MxArgs& a, const float* part, int64_t splits, int64_t n, hipStream_t st) {
+    // Tiles where they fill the chip: else eight threads a result read the parts side by side.
+    if (a.s >= 8 && ceil_div(n, 32) * ceil_div(a.s, 32) >= 512) {
+        const int64_t blocks = ceil_div(n, 32) * ceil_div(a.s, 32);
+        if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+        mx_join_tile_kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a, part, splits, n);
+        return hipGetLastError();
+    }
     const int64_t blocks = ceil_div(n, 32) * a.s;
     if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
     mx_join_kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a, part, splits, n);
@@ -714,7 +770,10 @@ bool mx_few_serves(const MxArgs& a) {
 }
 
 int64_t mx_few_workspace_bytes(const MxArgs& a) {
-    if (!a.trans) return few_plan(a).image_bytes;
+    if (!a.trans) {
+        const FewPlan p = few_plan(a);
+        return p.image_bytes + p.part_bytes;
+    }
     const int64_t splits = ceil_div(a.q, t_rows(a));
     return splits > 1 ? splits * a.s * a.r * 4 : 0;
 }
