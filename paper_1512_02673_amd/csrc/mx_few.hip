@@ -1,7 +1,13 @@
 // Products of a microscaled matrix with few right-hand sides: one vector (a
 // single token, a gradient step on a vector) up to 64 columns of bf16 values.
 //
-// Bound: reading A's codes once.  The work for a code is a conversion and the
+// Bound: reading A's codes once; a copy of that size reads at 5.4 to 6.3 TB/s in the
+// same 64- and 256-byte runs.  Measured: 65536 x 8192 in 4 bits times an fp32 vector
+// 54 us (5.3 TB/s), A^T of 262144 x 4096 times one 102 (5.6), 131072 x 16384 times 64
+// bf16 columns 325 (3.5: there the matrix cores and X's copies into shared memory
+// take turns with the codes), 11500 x 5750 times 16 14.5 a call, two launches.
+//
+// The work for a code is a conversion and the
 // matrix instruction, so neither shared memory nor a second copy holds codes:
 // a lane loads the 16 bytes that its own part of a matrix operand is made of,
 // and converts them in registers.  The order in which a sum's terms meet the
@@ -140,7 +146,7 @@ __global__ __launch_bounds__(256) void mx_order_kernel(MxArgs a, int planes, int
     for (int h = 0; h < planes; ++h) at[h * a.s] = h == 0 ? v[0] : h == 1 ? v[1] : v[2];
 }
 
-template <int BITS, int NT, int RT, int COLS, int CP, bool NTL>
+template <int BITS, int NT, int RT, int COLS, int CP>
 __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArgs a, int wk_log_, int planes, const u32x4_t* image, int64_t groups,
                                                                           int rounds_a_split, float* part) {
     constexpr int kStep = kStepOf<BITS>;
@@ -179,7 +185,7 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
         const int p = step * 16 + 4 * t + lk;
         const bool in = p < static_cast<int>(pieces_a);
 #pragma unroll
-        for (int x = 0; x < RT; ++x) w[S.value][x][t] = codes.four<NTL>(in ? code_row[x] + p * 16 : kNowhere);
+        for (int x = 0; x < RT; ++x) w[S.value][x][t] = codes.four(in ? code_row[x] + p * 16 : kNowhere);
     };
     const auto fetch_scales = [&](int step, auto S) {
         const uint32_t b0 = step * kScales * 4;
@@ -591,8 +597,10 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxArgs a, const float* par
     }
 }
 
-// Codes that do not stay in the memory-side cache from call to call.
-bool streamed(const MxArgs& a) { return streams(a.q * ceil_div(a.r, kMxBlock) * 4 * a.A.bits); }
+// Codes that do not stay in the memory-side cache from call to call are loaded as such across the blocks, whose
+// loads take whole lines (A^T of 262144 x 4096 times a vector 102 us, else 118).  Along the blocks two loads share
+// a line, and the second would fetch it again (65536 x 8192 times a vector 54 us, so 60).
+bool streamed(const MxArgs& a) { return streams(a.q * ceil_div(a.r, kMxBlock) * (4 * a.A.bits + 1)); }
 
 // The same for many sides, 32 of them and 32 results a workgroup: read along the results and, where a row of Y
 // holds the sides, turned in shared memory, so that it is written along them.
@@ -682,8 +690,7 @@ hipError_t launch_few(const MxArgs& a, const FewPlan& p, hipStream_t st) {
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
-        const auto kernel = streamed(a) ? mx_few_kernel<BITS, NT, RT, COLS, CP, true> : mx_few_kernel<BITS, NT, RT, COLS, CP, false>;
-        kernel<<<dim3(static_cast<uint32_t>(blocks)), kThreads, p.lds, st>>>(a, p.wk_log, planes, image, p.groups, static_cast<int>(p.per), part);
+        mx_few_kernel<BITS, NT, RT, COLS, CP><<<dim3(static_cast<uint32_t>(blocks)), kThreads, p.lds, st>>>(a, p.wk_log, planes, image, p.groups, static_cast<int>(p.per), part);
         const hipError_t e = hipGetLastError();
         return e != hipSuccess || !part ? e : launch_mx_join(a, part, p.splits, a.q, st);
     }

@@ -7,6 +7,11 @@
 // at most the format's largest value (a maximum between it and the next power
 // of two is cut down to it).  A block with an infinity or NaN in it gets the
 // NaN scale: all its values read back as NaN, and nothing hides the loss.
+//
+// Bound: memory.  Measured: 65536 x 8192 bf16 to 8 bits 330 to 350 us (1.62 GB, 4.6 to
+// 4.9 TB/s; a copy reaches 4.7) and back 280 to 295 (5.5 TB/s), 11500 x 5750 fp32 to 4
+// bits 61 us (4.9 TB/s) and back to bf16 26 (6.4).  Non-temporal loads and stores
+// were no faster.
 #include "mx.h"
 
 namespace coded {
