@@ -3,7 +3,7 @@
 //
 // Bound: reading A's codes once; a copy of that size reads at 5.4 to 6.3 TB/s in the
 // same 64- and 256-byte runs.  Measured: 65536 x 8192 in 4 bits times an fp32 vector
-// 54 us (5.3 TB/s), A^T of 262144 x 4096 times one 102 (5.6), 131072 x 16384 times 64
+// 50 us (5.7 TB/s), A^T of 262144 x 4096 times one 102 (5.6), 131072 x 16384 times 64
 // bf16 columns 325 (3.5: there the matrix cores and X's copies into shared memory
 // take turns with the codes), 11500 x 5750 times 16 14.5 a call, two launches.
 //
@@ -342,6 +342,182 @@ __global__ __launch_bounds__(kThreads, NT == 1 ? 4 : 2) void mx_few_kernel(MxArg
     }
 }
 
+// y = A x for one vector and long rows, on the vector units: a wave reads runs of 1 KB of four rows, a shape that
+// memory serves better than a matrix operand's sixteen rows of 64 bytes.  A lane's 16 bytes are values of one
+// block: a conversion a pair and a multiply-add a value, in fp32 with x in fp32, x's values read from shared
+// memory once for the four rows.  A row's scales come as a word a lane for kSpan runs and change lanes in registers:
+// loaded by the byte, with each run, those 6% of the bytes took 15% of the time.
+//
+// A workgroup takes `rows_wg` rows, its waves every eighth four of them, and goes over x in parts of
+// `pieces_staged` runs; a row's sums of the parts before wait in shared memory.
+//
+// Bound: reading A.  65536 x 8192 in 4 bits 50 to 52 us (5.6 TB/s; 6.3 between that and twice the rows, the rest is
+// the start), 65536 x 16384 95.6, 65536 x 4096 in 8 bits 45.1.  With two waves a SIMD in place of four 81.
+//
+// SIDE: where x comes from.  A contiguous fp32 or bf16 x is on its way before the first codes are (kFp32, kBf16:
+// whole words), others are loaded value by value (kAny).
+constexpr int kStaged = 16384;   // most columns of x in shared memory
+enum Side { kAny, kFp32, kBf16 };
+template <int BITS, bool NTL, Side SIDE>
+__global__ __launch_bounds__(kThreads, 4) void mx_vector_kernel(MxArgs a, int rows_wg, int pieces_staged) {
+    constexpr int V = 128 / BITS, kPiece = 64 * V, kRows = 4;   // values of a lane, columns of a run, rows of a wave
+    constexpr int kSpan = BITS;                                 // runs whose scales one word a lane holds
+    constexpr uint32_t kNowhere = 0xFFFFFFF0u;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    f32x4_t* xs = reinterpret_cast<f32x4_t*>(smem);   // [run][four values][lane]
+    float* sums = reinterpret_cast<float*>(smem + pieces_staged * kPiece * 4);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t row0 = blockIdx.x * static_cast<int64_t>(rows_wg);
+    const int fours = static_cast<int>(ceil_div(lesser(rows_wg, a.q - row0), kRows));
+    const int groups = fours > wave ? (fours - wave + kWaves - 1) / kWaves : 0;
+    const int64_t blocks = ceil_div(a.r, kMxBlock), row_bytes = blocks * 4 * BITS;
+    for (int64_t c0 = 0; c0 < a.r; c0 += static_cast<int64_t>(pieces_staged) * kPiece) {
+        const int pieces = static_cast<int>(lesser(pieces_staged, ceil_div(a.r - c0, kPiece)));
+        const bool last = c0 + static_cast<int64_t>(pieces) * kPiece >= a.r;
+        const int64_t code0 = c0 * BITS / 8, scale0 = c0 / kMxBlock;
+        u32x4_t w[2][kRows];
+        uint32_t sc[kRows], sc_next[kRows];
+        int next_group = 0, next_piece = 0;
+        const auto fetch = [&](auto S) {
+            const int64_t row = next_group < groups ? row0 + (wave + kWaves * next_group) * kRows : a.q;
+            const int64_t have = lesser(a.q - row, kRows) - 1;
+            const Window codes(a.A.codes + row * a.A.ldc + code0, have < 0 ? 0 : have * a.A.ldc + row_bytes - code0);
+            const uint32_t at = next_piece * 1024 + lane * 16;
+            const bool in = code0 + at < row_bytes;
+#pragma unroll
+            for (int e = 0; e < kRows; ++e)
+                w[S.value][e] = codes.four<NTL>(in ? at + e * static_cast<uint32_t>(a.A.ldc) : kNowhere);
+            if (++next_piece == pieces) {
+                next_piece = 0;
+                ++next_group;
+            }
+        };
+        // the scales of a span of runs, a word a lane
+        int span_group = 0, span = 0;
+        const auto fetch_scales = [&] {
+            const int64_t row = span_group < groups ? row0 + (wave + kWaves * span_group) * kRows : a.q;
+            const int64_t have = lesser(a.q - row, kRows) - 1, words = ceil_div(blocks, 4) * 4 - scale0;
+            const Window scales(a.A.scales + row * a.A.lds + scale0, have < 0 ? 0 : have * a.A.lds + words);
+            const uint32_t at = span * 256 + lane * 4;
+#pragma unroll
+            for (int e = 0; e < kRows; ++e) sc_next[e] = scales.word(at < words ? at + e * static_cast<uint32_t>(a.A.lds) : kNowhere);
+            if (++span * kSpan >= pieces) {
+                span = 0;
+                ++span_group;
+            }
+        };
+        typedef std::integral_constant<int, 0> even;
+        typedef std::integral_constant<int, 1> odd;
+        int piece = 0, group = 0;
+        constexpr int kCopies = kStaged / 4 / kThreads, kSize = SIDE == kBf16 ? 2 : 4;
+        u32x4_t xr[kCopies];
+        if constexpr (SIDE != kAny) {
+            const Window x(static_cast<const char*>(a.X) + c0 * kSize, (a.r - c0) * kSize);
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                const uint32_t from = (tid + i * kThreads) * 4 * kSize;
+                if constexpr (SIDE == kFp32) {
+                    xr[i] = x.four(from);
+                } else {
+                    const u32x2_t two = x.two(from);
+                    xr[i] = u32x4_t{two[0], two[1], 0u, 0u};
+                }
+            }
+        }
+        fetch_scales();
+        fetch(even{});
+        fetch(odd{});
+        __syncthreads();
+        if constexpr (SIDE != kAny) {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                const int c = (tid + i * kThreads) * 4, in = c % kPiece;
+                u32x4_t v = xr[i];
+                if constexpr (SIDE == kBf16) v = u32x4_t{v[0] << 16, v[0] & 0xFFFF0000u, v[1] << 16, v[1] & 0xFFFF0000u};
+                if (c < pieces * kPiece) xs[(c / kPiece * (V / 4) + in % V / 4) * 64 + in / V] = __builtin_bit_cast(f32x4_t, v);
+            }
+        } else {
+            for (int g = tid; g < pieces * (kPiece / 8); g += kThreads) {
+                u32x4_t v[3] = {};
+                load_side(a, 0, c0 + g * 8, a.r, v);
+                float f[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const auto plane = [&](int h) { return __uint_as_float(i & 1 ? v[h][i / 2] & 0xFFFF0000u : v[h][i / 2] << 16); };
+                    f[i] = plane(0) + (plane(1) + plane(2));   // the value again, exactly
+                }
+                const int in = g * 8 % kPiece;
+                f32x4_t* to = xs + (g * 8 / kPiece * (V / 4) + in % V / 4) * 64 + in / V;
+                to[0] = f32x4_t{f[0], f[1], f[2], f[3]};
+                to[64] = f32x4_t{f[4], f[5], f[6], f[7]};
+            }
+        }
+        __syncthreads();
+        float acc[kRows] = {};
+        const auto turn = [&](auto S) {
+            if (piece % kSpan == 0) {
+                // what lies behind the row's last scale counts as no number
+                const int64_t left = blocks - scale0 - piece * (kPiece / kMxBlock) - lane * 4;
+#pragma unroll
+                for (int e = 0; e < kRows; ++e) sc[e] = left >= 4 ? sc_next[e] : left <= 0 ? 0u : sc_next[e] & ((1u << (8 * left)) - 1);
+                fetch_scales();
+            }
+            float scale[kRows];
+            const int block = piece % kSpan * (kPiece / kMxBlock) + lane * V / kMxBlock;   // this lane's in the span
+#pragma unroll
+            for (int e = 0; e < kRows; ++e)
+                scale[e] = mx_scale(static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute(block & ~3, static_cast<int>(sc[e]))) >> (8 * (block & 3)) & 0xFFu);
+            const f32x4_t* at = xs + piece * (V / 4) * 64 + lane;
+#pragma unroll
+            for (int word = 0; word < 4; ++word) {
+                f32x4_t x[V / 16];
+#pragma unroll
+                for (int i = 0; i < V / 16; ++i) x[i] = at[(word * (V / 16) + i) * 64];
+#pragma unroll
+                for (int e = 0; e < kRows; ++e) {
+                    const auto pair = [&](auto P) {
+                        const mx_f32x2 v = mx_pair_f32<BITS, P.value>(w[S.value][e][word], scale[e]);
+                        acc[e] = fmaf(v.x, x[P.value / 2][P.value % 2 * 2], acc[e]);
+                        acc[e] = fmaf(v.y, x[P.value / 2][P.value % 2 * 2 + 1], acc[e]);
+                    };
+                    pair(std::integral_constant<int, 0>{});
+                    pair(std::integral_constant<int, 1>{});
+                    if constexpr (BITS == 4) {
+                        pair(std::integral_constant<int, 2>{});
+                        pair(std::integral_constant<int, 3>{});
+                    }
+                }
+            }
+            fetch(S);
+            if (++piece < pieces) return;
+            // the four rows' sums: half the lanes keep two rows, a quarter one, then the sixteen lanes of a row
+            const bool high = lane & 32, odd_row = lane & 16;
+            const float v0 = (high ? acc[2] : acc[0]) + __shfl_xor(high ? acc[0] : acc[2], 32, 64);
+            const float v1 = (high ? acc[3] : acc[1]) + __shfl_xor(high ? acc[1] : acc[3], 32, 64);
+            float v = (odd_row ? v1 : v0) + __shfl_xor(odd_row ? v0 : v1, 16, 64);
+#pragma unroll
+            for (int m = 8; m > 0; m /= 2) v += __shfl_xor(v, m, 64);
+            const int row = (wave + kWaves * group) * kRows + lane / 16;
+            if (lane % 16 == 0 && row0 + row < a.q) {
+                if (c0 > 0) v += sums[row];
+                if (last)
+                    mx_store(a, 0, row0 + row, v);
+                else
+                    sums[row] = v;
+            }
+#pragma unroll
+            for (int e = 0; e < kRows; ++e) acc[e] = 0.0f;
+            piece = 0;
+            ++group;
+        };
+        for (int i = 0; i < groups * pieces; i += 2) {
+            turn(even{});
+            if (i + 1 < groups * pieces) turn(odd{});
+        }
+    }
+}
+
 // ---------------------------------------------------------------- across the blocks
 
 // Z = A^T U.  A wave takes 16 bytes of 16 neighbouring lanes' columns and walks
@@ -597,9 +773,9 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxArgs a, const float* par
     }
 }
 
-// Codes that do not stay in the memory-side cache from call to call are loaded as such across the blocks, whose
-// loads take whole lines (A^T of 262144 x 4096 times a vector 102 us, else 118).  Along the blocks two loads share
-// a line, and the second would fetch it again (65536 x 8192 times a vector 54 us, so 60).
+// Codes that do not stay in the memory-side cache from call to call are loaded as such where loads take whole lines
+// (A^T of 262144 x 4096 times a vector 102 us, else 118; A of 65536 x 8192 53, else 57).  In mx_few_kernel two
+// loads share a line, and the second would fetch it again (65536 x 8192 54 us, so 60).
 bool streamed(const MxArgs& a) { return streams(a.q * ceil_div(a.r, kMxBlock) * (4 * a.A.bits + 1)); }
 
 // The same for many sides, 32 of them and 32 results a workgroup: read along the results and, where a row of Y
@@ -626,6 +802,23 @@ __global__ __launch_bounds__(256) void mx_join_tile_kernel(MxArgs a, const float
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (i0 + lo < a.s && j0 + hi + 8 * e < n) mx_store(a, i0 + lo, j0 + hi + 8 * e, tile[lo][hi + 8 * e]);
+}
+
+// One vector: mx_vector_kernel for rows of 2 KB of codes and more, or 1 KB where they do not stay in the memory-side
+// cache; few long rows are cut along the terms instead.  Measured, 4 bits, mx_few_kernel and mx_vector_kernel, us:
+// 65536 x 1024 11.5 14.5, x 2048 16.1 18.0, x 4096 28.0 28.3, x 8192 57.1 51.8, x 16384 117 95.6; 262144 x 1024 36.2
+// 45.8, x 2048 61.7 56.2; 4096 x 16384 19.3 15.7, x 40000 24.6 34.2, 8192 x 40000 42.8 43.3, 16384 x 40000 78.5 70.9.
+// An x that is loaded value by value, by every workgroup: up to 8192 columns, or where A takes longer (16384 x 16384,
+// every other value 38.2 and 47.4 us, 4-bit x 300 x 16384 17.3 and 11.0; 65536 x 8192 62.9 and 57.3).
+Side side_of(const MxArgs& a) {
+    if (!a.x_rows || a.x_bits || (a.x_bf16 && (reinterpret_cast<uintptr_t>(a.X) % 4 || a.r % 2))) return kAny;
+    return a.x_bf16 ? kBf16 : kFp32;
+}
+bool few_vector(const MxArgs& a) {
+    const int64_t row = a.r * a.A.bits / 8;
+    if (a.s != 1 || row < (streamed(a) ? 1024 : 2048)) return false;
+    const bool any = side_of(a) == kAny;
+    return a.r <= kStaged ? !any || a.r <= 8192 || streamed(a) : !any && a.q >= 8192;
 }
 
 int planes_of(const MxArgs& a) { return a.x_bits || a.x_bf16 ? 1 : 3; }
@@ -753,6 +946,30 @@ hipError_t launch_few_t(const MxArgs& a, hipStream_t st) {
     return launch_mx_join(a, part, splits, a.r, st);
 }
 
+// Two workgroups of mx_vector_kernel a compute unit.
+template <int BITS, bool NTL, Side SIDE>
+hipError_t launch_vector_side(const MxArgs& a, hipStream_t st) {
+    constexpr int kPiece = 64 * 128 / BITS;
+    const int64_t rows = std::min<int64_t>(4096, ceil_div(ceil_div(a.q, 512), 4) * 4);
+    const int64_t pieces = std::min<int64_t>(kStaged / kPiece, ceil_div(a.r, kPiece));
+    const int64_t blocks = ceil_div(a.q, rows), lds = pieces * kPiece * 4 + (a.r > pieces * kPiece ? rows * 4 : 0);
+    if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
+    mx_vector_kernel<BITS, NTL, SIDE><<<dim3(static_cast<uint32_t>(blocks)), kThreads, lds, st>>>(a, static_cast<int>(rows), static_cast<int>(pieces));
+    return hipGetLastError();
+}
+
+template <int BITS>
+hipError_t launch_vector(const MxArgs& a, hipStream_t st) {
+    const Side side = side_of(a);
+    if (streamed(a))
+        return side == kAny    ? launch_vector_side<BITS, true, kAny>(a, st)
+               : side == kFp32 ? launch_vector_side<BITS, true, kFp32>(a, st)
+                               : launch_vector_side<BITS, true, kBf16>(a, st);
+    return side == kAny    ? launch_vector_side<BITS, false, kAny>(a, st)
+           : side == kFp32 ? launch_vector_side<BITS, false, kFp32>(a, st)
+                           : launch_vector_side<BITS, false, kBf16>(a, st);
+}
+
 }  // namespace
 
 hipError_t launch_mx_join(const MxArgs& a, const float* part, int64_t splits, int64_t n, hipStream_t st) {
@@ -778,6 +995,7 @@ bool mx_few_serves(const MxArgs& a) {
 
 int64_t mx_few_workspace_bytes(const MxArgs& a) {
     if (!a.trans) {
+        // whatever way x lies: the sizes alone say how much, also where mx_vector_kernel needs none
         const FewPlan p = few_plan(a);
         return p.image_bytes + p.part_bytes;
     }
@@ -792,6 +1010,7 @@ hipError_t launch_mx_few(const MxArgs& args, hipStream_t st) {
         a.ldx = a.trans ? a.q : a.r;
     }
     if (a.trans) return a.A.bits == 4 ? launch_few_t<4>(a, st) : launch_few_t<8>(a, st);
+    if (few_vector(a)) return a.A.bits == 4 ? launch_vector<4>(a, st) : launch_vector<8>(a, st);
     return a.A.bits == 4 ? launch_few_cols<4>(a, st) : launch_few_cols<8>(a, st);
 }
 

@@ -519,3 +519,34 @@ def test_rows_of_more_than_eight_megabytes(lib, torch):
     Z = torch.empty((r, 2), device="cuda")
     lib.coded_mx_mm_t(M, U, Z)
     assert torch.equal(Z.double(), A.t() @ U.double())
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("x", ["f32", "bf16", "mx4", "mx8"])
+def test_one_vector_and_long_rows(lib, torch, bits, x):
+    rng = np.random.default_rng(31)
+    for q, r, order, whole in [(4096, 2048, 3, True), (4099, 2050, 1, False), (20485, 2081, 0, True), (4103, 16384, 3, True), (4130, 16417, 2, True),
+                               (4097, 33001, 1, True)]:
+        check_product(lib, torch, rng, False, q, r, 1, bits, x, "bf16" if order == 1 and not whole else "f32", bool(order & 1) or x.startswith("mx"),
+                      bool(order & 2), pad=order, alpha=-1.0, beta=0.0 if whole else 0.5, whole=whole)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("r", [2050, 18000])
+def test_no_number_in_a_long_row_spreads_to_no_other(lib, torch, bits, r):
+    rng = np.random.default_rng(33)
+    q = 4100
+    M, A = microscaled(lib, torch, rng, q, r, bits)
+    M.scales[77, (r - 1) // 32] = 255
+    M.scales[q - 1, 0] = 255
+    x = torch.randn(r, device="cuda")
+    Y = torch.empty(q, device="cuda")
+    lib.coded_mx_mm(M, x, Y)
+    bad = np.isnan(host(Y))
+    assert bad.sum() == 2 and bad[77] and bad[q - 1]
+    x[r - 1] = float("inf")
+    lib.coded_mx_mm(M, x, Y)
+    last = A[:, r - 1].copy()
+    last[[77, q - 1]] = 0.0          # 0 times an infinity, like NaN times it, is NaN
+    got = host(Y)
+    assert np.array_equal(np.isnan(got), last == 0) and np.array_equal(got[last != 0], np.copysign(np.inf, last[last != 0]))
