@@ -550,3 +550,20 @@ def test_no_number_in_a_long_row_spreads_to_no_other(lib, torch, bits, r):
     last[[77, q - 1]] = 0.0          # 0 times an infinity, like NaN times it, is NaN
     got = host(Y)
     assert np.array_equal(np.isnan(got), last == 0) and np.array_equal(got[last != 0], np.copysign(np.inf, last[last != 0]))
+
+
+@pytest.mark.parametrize("q,r", [(4100, 4100), (4099, 8190), (262144, 2050), (32768, 16390), (33001, 16384)])
+def test_one_vector_however_it_lies(lib, torch, q, r):
+    """fp32 and bf16, contiguous, at every bf16 address, and strided; matrices below and above 256 MB."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    codes, scales, A = whole_codes(torch, q, r, g)
+    M = lib.MXMatrix(codes, scales, r, lib.CODED_MX4)
+    for dtype in (torch.float32, torch.bfloat16):
+        for off, step in ((0, 1), (1, 1), (2, 1), (3, 2)):
+            flat = torch.full((off + r * step + 8,), float("nan"), dtype=dtype, device="cuda")
+            X = flat[off:off + r * step].view(r, step)[:, :1]
+            X.copy_(torch.randint(-7, 8, (r, 1), device="cuda", generator=g))
+            wide = torch.full((q + 2, 1), 7.0, device="cuda")
+            lib.coded_mx_mm(M, X, wide[1:-1])
+            assert torch.equal(wide[1:-1].double(), A @ X.double()), (dtype, off, step)
+            assert wide[0] == 7 and wide[-1] == 7
