@@ -94,7 +94,9 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     const int64_t s_all = (a.q - 1) * a.A.lds + (TRANS ? blocks : ceil_div(blocks, 4) * 4) - s_skip;
     const int64_t plane = t0 > 0 ? t0 / g.steps : 0, p_step = PT ? kStep * g.pitch : kStep;
     const uint16_t* p_base = g.P + plane * g.plane + (PT ? i0 : i0 * g.pitch) + step * p_step;
-    const int64_t p_all = PT ? (g.row - 1) * g.pitch + a.s - i0 : (a.s - i0 - 1) * g.pitch + g.row;
+    // By columns the bound is a whole number of words, as loads are: with an odd number of sides the last word holds the
+    // last side and one element more, which belongs to no side (rows start at words, so it is in the last row's word).
+    const int64_t p_all = PT ? ((g.row - 1) * g.pitch + a.s - i0 + 1) / 2 * 2 : (a.s - i0 - 1) * g.pitch + g.row;
     int64_t p_left = (p_all - step * p_step) * 2;
     const uint8_t *q_base = a.A.codes + q_skip + step * q_step, *s_base = a.A.scales + s_skip + step * s_step;
     int64_t q_left = q_all - step * q_step, s_left = s_all - step * s_step;

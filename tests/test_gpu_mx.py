@@ -567,3 +567,38 @@ def test_one_vector_however_it_lies(lib, torch, q, r):
             lib.coded_mx_mm(M, X, wide[1:-1])
             assert torch.equal(wide[1:-1].double(), A @ X.double()), (dtype, off, step)
             assert wide[0] == 7 and wide[-1] == 7
+
+
+def whole_codes_of(torch, bits, rows, cols, g):
+    """whole_codes in 4 or 8 bits (whole numbers up to 8 there)."""
+    if bits == 4:
+        return whole_codes(torch, rows, cols, g)
+    values = om.format_values(8)
+    table = torch.tensor([c for c, v in enumerate(values) if np.isfinite(v) and v == round(v) and abs(v) <= 8], device="cuda", dtype=torch.uint8)
+    codes = table[torch.randint(0, len(table), (rows, -(-cols // 32) * 32), device="cuda", generator=g)]
+    codes[:, cols:] = 0
+    v = torch.tensor(values, device="cuda")[codes.int()][:, :cols]
+    return codes, torch.full((rows, -(-cols // 128) * 4), 127, dtype=torch.uint8, device="cuda"), v
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_an_odd_number_of_columns_of_x_in_even_rows(lib, torch, transposed, bits):
+    """bf16 columns that are read as they are: with s odd the last row's last word holds the last side's term and
+    nothing else of X.  That row is made of numbers that every last side's result shows."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for n, k, s in ((300, 1, 67), (700, 300, 131), (90, 3, 67), (260, 64, 65), (8200, 130, 1101), (130, 65, 8191), (8200, 128, 1027)):
+        q, r = (k, n) if transposed else (n, k)
+        codes, scales, A = whole_codes_of(torch, bits, q, r, g)
+        M = lib.MXMatrix(codes, scales, r, fmt_of(lib, bits))
+        A = A.t() if transposed else A
+        for ld, off in ((s + 1, 0), (s + 1, 2), (s + 7, 4)):
+            flat = torch.full((off + (k - 1) * ld + s,), float("nan"), dtype=torch.bfloat16, device="cuda")
+            X = flat[off:].as_strided((k, s), (ld, 1))
+            X.copy_(torch.randint(-7, 8, (k, s), device="cuda", generator=g))
+            X[k - 1].fill_(9)
+            for y_rows in (False, True):
+                Y = torch.empty((s, n) if y_rows else (n, s), device="cuda")
+                (lib.coded_mx_mm_t if transposed else lib.coded_mx_mm)(M, X, Y, y_rows=y_rows)
+                want = A @ X.double()
+                assert torch.equal(Y.double(), want.t() if y_rows else want), (n, k, s, ld, off, y_rows)
