@@ -675,10 +675,13 @@ def _mx_product(transposed, M, X, Y, x_rows, y_rows, alpha, beta, C, workspace, 
     if isinstance(workspace, str):
         wsb = coded_mx_workspace(transposed, M.fmt, q, r, x_dt, s, x_rows, y_rows)
         if wsb:
-            workspace = _torch().empty(wsb, dtype=_torch().uint8, device=Y.device)
+            torch = _torch()
+            if stream is None:
+                workspace = torch.empty(wsb, dtype=torch.uint8, device=Y.device)
+            else:   # memory of that stream's own: the current stream's may still be in use by what waits there
+                with torch.cuda.stream(stream):
+                    workspace = torch.empty(wsb, dtype=torch.uint8, device=Y.device)
             wsp = workspace.data_ptr()
-            if stream is not None:   # its memory is not handed out again before that stream is done with it
-                workspace.record_stream(stream)
     elif workspace is not None:
         wsp, wsb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     order = bool(x_rows) | bool(y_rows) << 1

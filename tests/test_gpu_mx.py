@@ -602,3 +602,30 @@ def test_an_odd_number_of_columns_of_x_in_even_rows(lib, torch, transposed, bits
                 (lib.coded_mx_mm_t if transposed else lib.coded_mx_mm)(M, X, Y, y_rows=y_rows)
                 want = A @ X.double()
                 assert torch.equal(Y.double(), want.t() if y_rows else want), (n, k, s, ld, off, y_rows)
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+def test_workspace_on_another_stream_leaves_the_current_ones_memory_alone(lib, torch, transposed):
+    """A tensor that is let go of while work on the current stream has still to read it; a product on another stream
+    whose workspace is as large comes meanwhile."""
+    rng = np.random.default_rng(14)
+    q, r, s = (60000, 512, 4) if transposed else (200, 40000, 9)
+    M, A = microscaled(lib, torch, rng, q, r, 4, whole=True)
+    A = A.T if transposed else A
+    x = rng.integers(-5, 6, (A.shape[1], s)).astype(np.float32)
+    X, Y = torch.from_numpy(x).cuda(), torch.empty((A.shape[0], s), device="cuda")
+    call = lib.coded_mx_mm_t if transposed else lib.coded_mx_mm
+    need = lib.coded_mx_workspace(transposed, M.fmt, q, r, lib.CODED_F32, s)
+    assert need > 0
+    side = torch.cuda.Stream()
+    out = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    held = torch.full((need,), 7, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)     # some tens of milliseconds
+    out.copy_(held)
+    del held
+    call(M, X, Y, stream=side)
+    side.synchronize()
+    assert np.array_equal(host(Y), A @ x)
+    torch.cuda.synchronize()
+    assert bool((out == 7).all())

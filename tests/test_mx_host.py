@@ -1,7 +1,9 @@
 """Microscaled matrices, what needs no GPU: the oracle's format, the pitches, and every refusal
 (all of them are found on the host before anything is launched)."""
+import contextlib
 import ctypes
 import math
+import types
 
 import numpy as np
 import pytest
@@ -157,3 +159,59 @@ def test_binding_refuses_wrong_tensors(lib):
         lib.coded_mx_quantize(f(6, 41), M)
     with pytest.raises(ValueError):
         lib.coded_mx_dequantize(M, f(5, 40))
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+def test_workspace_of_a_call_on_a_stream_is_that_streams(lib, monkeypatch, transposed):
+    """Memory handed out for the current stream may still be read or written by work that waits there, which a kernel
+    on another stream does not wait for: the automatic workspace is asked for with the call's stream as the current one."""
+    torch = pytest.importorskip("torch")
+    q, r, s = (100000, 512, 2) if transposed else (512, 40000, 9)
+    assert lib.coded_mx_workspace(transposed, lib.CODED_MX4, q, r, lib.CODED_F32, s) > 0
+    M = lib.alloc_mx(q, r, lib.CODED_MX4, device="cpu")
+    k, n = (q, r) if transposed else (r, q)
+    X, Y = torch.empty((k, s)), torch.empty((n, s))
+
+    class Buffer:
+        def data_ptr(self):
+            return 0x1000
+
+        def record_stream(self, stream):
+            pass
+
+    class Torch:
+        uint8 = torch.uint8
+        current = None
+        asked = []
+
+        def empty(self, *a, **k):
+            self.asked.append(self.current)
+            return Buffer()
+
+        @property
+        def cuda(self):
+            outer = self
+
+            class Cuda:
+                @staticmethod
+                @contextlib.contextmanager
+                def stream(s):
+                    outer.current, before = s, outer.current
+                    yield
+                    outer.current = before
+            return Cuda
+
+    real = lib.lib()
+
+    class Library:
+        coded_mx_workspace = real.coded_mx_workspace
+
+        def __getattr__(self, name):
+            return lambda *a: lib.CODED_OK
+
+    fake, side = Torch(), types.SimpleNamespace(cuda_stream=7)
+    lib._dtype_code(X)
+    monkeypatch.setattr(lib, "_torch", lambda: fake)
+    monkeypatch.setattr(lib, "lib", Library)
+    (lib.coded_mx_mm_t if transposed else lib.coded_mx_mm)(M, X, Y, stream=side)
+    assert fake.asked == [side] and fake.current is None
