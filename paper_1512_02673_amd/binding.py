@@ -7,6 +7,7 @@ library has not been built.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -175,6 +176,12 @@ def _stream(stream=None):
     return raw(torch.cuda.current_device())
 
 
+def _memory_of(stream):
+    """Within it torch hands out memory of `stream` (None: the current one): memory of the current
+    stream's may still be in use by what waits there, and another stream does not wait for that."""
+    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
+
+
 _DTYPE_CODES: dict = {}   # filled on first use: torch is imported late
 
 
@@ -306,7 +313,8 @@ def coded_encode_worker_mm(code: Code, A, parity, X, Y, workspace="auto", stream
     if rx != r:
         raise ValueError("X must have r rows")
     if isinstance(workspace, str):
-        workspace = worker_workspace(code, A, X)
+        with _memory_of(stream):
+            workspace = worker_workspace(code, A, X)
     _check(lib().coded_encode_worker_mm(code.handle, _dtype_code(A), _ptr(A), q, r, lda, _ptr(parity), _ptr(X), s,
                                         ldx, _ptr(Y), _dtype_code(Y), _ptr(workspace), _stream(stream)))
 
@@ -375,7 +383,8 @@ def coded_straggler_matmul(code: Code, A, parity, X, Y, out, info, seed: int, dr
         raise ValueError("X must have r rows")
     _, so, ldo = _matrix(out, "out")
     if isinstance(workspace, str):
-        workspace = worker_workspace(code, A, X)
+        with _memory_of(stream):
+            workspace = worker_workspace(code, A, X)
     surv = np.zeros(code.k, dtype=np.int32)
     timeline = np.zeros((code.n, 3), dtype=np.float64)
     lat = ctypes.c_double()
@@ -676,11 +685,8 @@ def _mx_product(transposed, M, X, Y, x_rows, y_rows, alpha, beta, C, workspace, 
         wsb = coded_mx_workspace(transposed, M.fmt, q, r, x_dt, s, x_rows, y_rows)
         if wsb:
             torch = _torch()
-            if stream is None:
+            with _memory_of(stream):
                 workspace = torch.empty(wsb, dtype=torch.uint8, device=Y.device)
-            else:   # memory of that stream's own: the current stream's may still be in use by what waits there
-                with torch.cuda.stream(stream):
-                    workspace = torch.empty(wsb, dtype=torch.uint8, device=Y.device)
             wsp = workspace.data_ptr()
     elif workspace is not None:
         wsp, wsb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
