@@ -380,9 +380,12 @@ hipError_t launch_bits(const MxArgs& a, const TileArgs& g, const Plan& p, hipStr
 
 }  // namespace
 
-// Offsets within a tile's rows, of X and of codes, are 32-bit.
+// Offsets within a tile's rows, of X and of codes, are 32-bit.  Two 4-bit matrices with rows of X further apart than
+// mx_scaled_kernel takes go to the general kernel: the workspace is asked for by sizes, and by those that product
+// has none for an X in bf16.
 bool mx_tiled_serves(const MxArgs& a) {
     const int64_t most = (int64_t(1) << 31) / 256;
+    if (a.x_bits == 4 && a.A.bits == 4) return false;
     return (a.trans ? a.q : a.r) < most / 2 && std::max(a.A.ldc, a.A.lds) < most && (!a.x_rows || a.ldx < most / 2);
 }
 

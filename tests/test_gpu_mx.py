@@ -629,3 +629,25 @@ def test_workspace_on_another_stream_leaves_the_current_ones_memory_alone(lib, t
     assert np.array_equal(host(Y), A @ x)
     torch.cuda.synchronize()
     assert bool((out == 7).all())
+
+
+@pytest.mark.parametrize("x_bits", [4, 8])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("far", ["codes", "scales"])
+def test_microscaled_rows_of_x_eight_megabytes_apart(lib, torch, bits, x_bits, far):
+    """Every so many rows of a long saved batch: the workspace of the query by sizes is enough at any pitch of X."""
+    g = torch.Generator(device="cuda").manual_seed(15)
+    n, k, s = 300, 200, 70
+    codes, scales, A = whole_codes_of(torch, bits, n, k, g)
+    M = lib.MXMatrix(codes, scales, k, fmt_of(lib, bits))
+    xc, xs, X64 = whole_codes_of(torch, x_bits, s, k, g)
+    wide = torch.empty((s, 1 << 23), dtype=torch.uint8, device="cuda")
+    near = xc if far == "codes" else xs
+    wide[:, :near.shape[1]] = near
+    view = wide[:, :near.shape[1]]
+    X = lib.MXMatrix(view if far == "codes" else xc, xs if far == "codes" else view, k, fmt_of(lib, x_bits))
+    for y_rows in (False, True):
+        Y = torch.empty((s, n) if y_rows else (n, s), device="cuda")
+        lib.coded_mx_mm(M, X, Y, x_rows=True, y_rows=y_rows)
+        want = A @ X64.t()
+        assert torch.equal(Y.double(), want.t() if y_rows else want)
