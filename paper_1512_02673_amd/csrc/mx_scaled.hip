@@ -26,8 +26,9 @@ constexpr int kStep = 128;   // terms: four blocks
 struct ScaledArgs {
     int64_t steps;
     Cut cut;
-    float* part;     // sums of the shared tiles' splits, or null
-    int32_t flush;   // as in mx_tiled.hip
+    int64_t first;   // these three as in mx_tiled.hip
+    float* sums;
+    int32_t flush;
 };
 
 // The rows of codes and scales that one side of a tile takes of a step.
@@ -89,7 +90,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_scaled_kernel(MxArgs a, Scaled
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wi = (wave & 1) * TI * 16, wj = (wave >> 1) * TJ * 16;
     const int64_t blocks = ceil_div(a.r, kMxBlock);
-    const TilePlace place = tile_place(g.cut);
+    const TilePlace place = tile_place(g.cut, g.first + blockIdx.x);
     const int64_t i0 = place.i * BI, j0 = place.j * BJ;
 
     PX px;
@@ -114,9 +115,10 @@ __global__ __launch_bounds__(kThreads, 2) void mx_scaled_kernel(MxArgs a, Scaled
                                   : __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(xv[x], av, acc[x][y], kE2M1, kE2M1, 0, xe[x], 0, ae);
         }
     };
-    float* part = place.split < 0 ? nullptr : g.part + (place.split * g.cut.rest() + place.shared) * (BI * BJ);
+    const bool whole = place.split < 0;
+    float* const sums = g.sums + (whole ? blockIdx.x : g.cut.slots + place.split * g.cut.rest() + place.shared) * (BI * BJ);
     // as in mx_tile_kernel
-    const auto put = [&](bool first) {
+    const auto put = [&](bool first, bool last) {
         int at = tid;
         asm volatile("" : "+v"(at));
         const int l15 = at & 15, l4 = (at >> 4 & 3) * 4;
@@ -125,10 +127,12 @@ __global__ __launch_bounds__(kThreads, 2) void mx_scaled_kernel(MxArgs a, Scaled
 #pragma unroll
             for (int y = 0; y < TJ; ++y) {
                 const int ti = wi + 16 * x + (YROWS ? l15 : l4), tj = wj + 16 * y + (YROWS ? l4 : l15);
-                if (part)
-                    *reinterpret_cast<f32x4_t*>(part + (YROWS ? ti * BJ + tj : tj * BI + ti)) = acc[x][y];
+                f32x4_t* so_far = reinterpret_cast<f32x4_t*>(sums + (YROWS ? ti * BJ + tj : tj * BI + ti));
+                if (!first) acc[x][y] += *so_far;
+                if (whole && last)
+                    store_four<YROWS>(a, a.q, i0 + ti, j0 + tj, acc[x][y]);
                 else
-                    store_four<YROWS>(a, a.q, i0 + ti, j0 + tj, acc[x][y], first);
+                    *so_far = acc[x][y];
                 acc[x][y] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
     };
@@ -148,7 +152,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_scaled_kernel(MxArgs a, Scaled
         stage();
     }
     for (bool first = true;; first = false) {
-        const int64_t end = g.flush && !part ? lesser(t + g.flush, t1) : t1;
+        const int64_t end = g.flush && whole ? lesser(t + g.flush, t1) : t1;
         for (; t < end; ++t) {
             __syncthreads();
             if (t + 1 < t1) fetch(t + 1);
@@ -156,12 +160,12 @@ __global__ __launch_bounds__(kThreads, 2) void mx_scaled_kernel(MxArgs a, Scaled
             __syncthreads();
             if (t + 1 < t1) stage();
         }
-        put(first);
+        put(first, t >= t1);
         if (t >= t1) break;
     }
 }
 
-Cut cut_of(const MxArgs& a) { return cut_tiles(a.s, a.q, ceil_div(a.r, kStep)); }
+Cut cut_of(const MxArgs& a) { return cut_tiles(a.s, a.q, ceil_div(a.r, kStep), kChain / kStep); }
 
 }  // namespace
 
@@ -172,7 +176,7 @@ bool mx_scaled_serves(const MxArgs& a) {
 }
 
 int64_t mx_scaled_workspace_bytes(const MxArgs& a) {
-    return cut_of(a).part_bytes();
+    return cut_of(a).sums_bytes();
 }
 
 hipError_t launch_mx_scaled(const MxArgs& a, hipStream_t st) {
@@ -180,16 +184,18 @@ hipError_t launch_mx_scaled(const MxArgs& a, hipStream_t st) {
     ScaledArgs g{};
     g.steps = ceil_div(a.r, kStep);
     g.cut = c;
-    g.part = c.splits > 1 ? static_cast<float*>(a.workspace) : nullptr;
-    g.flush = a.y_bf16 ? 0 : 16384 / kStep;
+    g.sums = static_cast<float*>(a.workspace);
+    g.flush = a.y_bf16 ? 0 : kChain / kStep;
     if (!grid_fits(c.groups(), kThreads)) return hipErrorInvalidConfiguration;
-    const dim3 grid(static_cast<uint32_t>(c.groups()));
     const auto kernel = c.large ? (a.y_rows ? mx_scaled_kernel<4, 8, true> : mx_scaled_kernel<4, 8, false>)
                                 : (a.y_rows ? mx_scaled_kernel<2, 4, true> : mx_scaled_kernel<2, 4, false>);
-    kernel<<<grid, kThreads, 0, st>>>(a, g);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !g.part) return e;
-    return launch_shared_tiles(a, c, g.part, a.q, st);
+    const hipError_t e = over_groups(c, [&](int64_t first, int64_t groups) {
+        g.first = first;
+        kernel<<<dim3(static_cast<uint32_t>(groups)), kThreads, 0, st>>>(a, g);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess || c.splits <= 1) return e;
+    return launch_shared_tiles(a, c, g.sums, a.q, st);
 }
 
 }  // namespace coded

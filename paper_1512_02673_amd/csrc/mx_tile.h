@@ -10,17 +10,23 @@ namespace coded {
 namespace {
 
 constexpr int kThreads = 256;   // of a tile's workgroup: two waves along each of its sides
+constexpr int kChain = 16384;   // terms added up in registers before the sums move to memory
 // How many right-hand sides and results a tile has, and which tiles' sums are shared by several workgroups: the
 // first `whole` tiles are one workgroup's each, the rest are split along the terms.
 struct Cut {
     bool large;                        // 128 x 256, else 64 x 128
     int64_t tiles_i, tiles_j, whole;
     int64_t splits, per;               // of each of the other tiles, and steps of a split
+    int64_t slots;                     // whole tiles of a launch, where they have more terms than a chain: else 0
     __host__ __device__ int64_t rest() const { return tiles_i * tiles_j - whole; }
     __host__ __device__ int64_t groups() const { return whole + rest() * splits; }
+    int64_t tile_bytes() const { return (large ? 128 * 256 : 64 * 128) * 4; }
     // fp32 sums of every split of every shared tile, [split][tile][place in the tile, as Y is ordered]
-    int64_t part_bytes() const { return splits > 1 ? rest() * splits * (large ? 128 * 256 : 64 * 128) * 4 : 0; }
+    int64_t part_bytes() const { return splits > 1 ? rest() * splits * tile_bytes() : 0; }
+    // those, behind the whole tiles' sums of the chains so far (likewise ordered in the tile)
+    int64_t sums_bytes() const { return slots * tile_bytes() + part_bytes(); }
 };
+constexpr int64_t kSlotBytes = int64_t(256) << 20;   // of one launch's whole tiles: four rounds of them
 // Microseconds of one step of each of `groups` workgroups at once, as measured (64 terms, bf16): one to a compute
 // unit, two, and as many as there are.
 inline double step_us(bool large, int64_t groups) {
@@ -33,7 +39,8 @@ inline double step_us(bool large, int64_t groups) {
 // 16, and small ones): 512 x 4096 of 4096 terms 86 57 41 46 68, 47 41 42 52 70 us; 578 x 6075 of 71240 terms in
 // three planes 4321 2249 1874 1885 1892, 3043 3186 3323 3249 2682; 1000 x 1000 of 16384 terms 307 166 92 63 62,
 // 163 95 67 68 72.
-inline Cut cut_tiles(int64_t s, int64_t n, int64_t steps) {
+// `chain`: steps of a chain.
+inline Cut cut_tiles(int64_t s, int64_t n, int64_t steps, int64_t chain) {
     Cut best{};
     double best_us = -1;
     for (int large = 1; large >= 0; --large) {
@@ -55,7 +62,20 @@ inline Cut cut_tiles(int64_t s, int64_t n, int64_t steps) {
             }
         }
     }
+    if (steps > chain) best.slots = std::min(best.whole, kSlotBytes / best.tile_bytes());
     return best;
+}
+
+// f(first workgroup, workgroups) for as many launches as there are fillings of the slots.
+template <class F>
+hipError_t over_groups(const Cut& c, F f) {
+    int64_t first = 0;
+    if (c.slots)
+        for (; c.whole - first > c.slots; first += c.slots) {
+            const hipError_t e = f(first, c.slots);
+            if (e != hipSuccess) return e;
+        }
+    return f(first, c.groups() - first);
 }
 
 // Which tile a workgroup takes, and which split of its terms (-1: all of them).  Workgroups go to the eight XCDs in
@@ -68,8 +88,7 @@ __device__ __forceinline__ TilePlace place_of(const Cut& c, int64_t id) {
     const int64_t strip = id / (8 * c.tiles_j), in = id % (8 * c.tiles_j), high = lesser(8, c.tiles_i - strip * 8);
     return {strip * 8 + in % high, in / high, -1, 0};
 }
-__device__ __forceinline__ TilePlace tile_place(const Cut& c) {
-    const int64_t b = blockIdx.x;
+__device__ __forceinline__ TilePlace tile_place(const Cut& c, int64_t b) {
     if (b >= c.whole) {
         const int64_t rest = c.rest(), r = b - c.whole;
         TilePlace p = place_of(c, c.whole + r % rest);
@@ -93,12 +112,12 @@ __device__ __forceinline__ int row_group(int row) {
 
 // A result's tile of four: results j .. j + 3 of side i (YROWS), or result j of sides i .. i + 3.
 template <bool YROWS>
-__device__ __forceinline__ void store_four(const MxArgs& a, int64_t n, int64_t i, int64_t j, f32x4_t v, bool first) {
+__device__ __forceinline__ void store_four(const MxArgs& a, int64_t n, int64_t i, int64_t j, f32x4_t v) {
     const int64_t have = YROWS ? n - j : a.s - i;
     if (have <= 0 || (YROWS ? i >= a.s : j >= n)) return;
     const int64_t at = YROWS ? i * a.ldy + j : j * a.ldy + i, ct = YROWS ? i * a.ldcc + j : j * a.ldcc + i;
     v *= a.alpha;
-    if (a.C && first) {
+    if (a.C) {
         float c[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -124,36 +143,35 @@ __device__ __forceinline__ void store_four(const MxArgs& a, int64_t n, int64_t i
     } else {
         float* y = static_cast<float*>(a.Y) + at;
         if (have >= 4) {
-            if (!first) v += *reinterpret_cast<const f32x4_any*>(y);
             *reinterpret_cast<f32x4_any*>(y) = v;
         } else {
 #pragma unroll
             for (int e = 0; e < 3; ++e)
-                if (e < have) y[e] = first ? v[e] : y[e] + v[e];
+                if (e < have) y[e] = v[e];
         }
     }
 }
 
 // The shared tiles' results from the sums of their splits, added in order.  A workgroup takes 1024 places of a tile.
 template <int BI, int BJ, bool YROWS>
-__global__ __launch_bounds__(kThreads) void mx_shared_tiles_kernel(MxArgs a, Cut c, const float* part, int64_t n) {
+__global__ __launch_bounds__(kThreads) void mx_shared_tiles_kernel(MxArgs a, Cut c, const float* sums, int64_t n) {
     constexpr int kParts = BI * BJ / (4 * kThreads);
     const int64_t tile = blockIdx.x / kParts;
     const int at = (static_cast<int>(blockIdx.x % kParts) * kThreads + threadIdx.x) * 4;
     const TilePlace p = place_of(c, c.whole + tile);
-    const float* from = part + tile * (BI * BJ) + at;
+    const float* from = sums + (c.slots + tile) * (BI * BJ) + at;
     f32x4_t v = *reinterpret_cast<const f32x4_t*>(from);
     for (int64_t k = 1; k < c.splits; ++k) v += *reinterpret_cast<const f32x4_t*>(from + k * c.rest() * (BI * BJ));
     const int64_t i = p.i * BI + (YROWS ? at / BJ : at % BI), j = p.j * BJ + (YROWS ? at % BJ : at / BI);
-    store_four<YROWS>(a, n, i, j, v, true);
+    store_four<YROWS>(a, n, i, j, v);
 }
 
-inline hipError_t launch_shared_tiles(const MxArgs& a, const Cut& c, const float* part, int64_t n, hipStream_t st) {
+inline hipError_t launch_shared_tiles(const MxArgs& a, const Cut& c, const float* sums, int64_t n, hipStream_t st) {
     const int64_t blocks = c.rest() * ((c.large ? 128 * 256 : 64 * 128) / (4 * kThreads));
     if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
     const auto kernel = c.large ? (a.y_rows ? mx_shared_tiles_kernel<128, 256, true> : mx_shared_tiles_kernel<128, 256, false>)
                                 : (a.y_rows ? mx_shared_tiles_kernel<64, 128, true> : mx_shared_tiles_kernel<64, 128, false>);
-    kernel<<<dim3(static_cast<uint32_t>(blocks)), kThreads, 0, st>>>(a, c, part, n);
+    kernel<<<dim3(static_cast<uint32_t>(blocks)), kThreads, 0, st>>>(a, c, sums, n);
     return hipGetLastError();
 }
 

@@ -39,7 +39,8 @@ struct TileArgs {
     int32_t planes;
     int64_t steps;              // of one plane
     Cut cut;
-    float* part;                // sums of the shared tiles' splits, or null
+    int64_t first;              // workgroup of this launch among all
+    float* sums;                // whole tiles' sums of the chains so far, then those of the shared tiles' splits
     int32_t flush;              // steps summed in one chain (fp32 results), 0: all
 };
 
@@ -75,7 +76,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     const int64_t n = TRANS ? a.r : a.q;
     const int64_t blocks = ceil_div(a.r, kMxBlock), code_row = blocks * 4 * BITS;
 
-    const TilePlace place = tile_place(g.cut);
+    const TilePlace place = tile_place(g.cut, g.first + blockIdx.x);
     const int64_t i0 = place.i * BI, j0 = place.j * BJ;
 
     // what this thread loads of a step: byte offsets in the tile's rows
@@ -249,9 +250,10 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
             }
         }
     };
-    float* part = place.split < 0 ? nullptr : g.part + (place.split * g.cut.rest() + place.shared) * (BI * BJ);
+    const bool whole = place.split < 0;
+    float* const sums = g.sums + (whole ? blockIdx.x : g.cut.slots + place.split * g.cut.rest() + place.shared) * (BI * BJ);
     // the lane's place in the tile, computed anew each time: kept, its addresses would take registers from the sums
-    const auto put = [&](bool first) {
+    const auto put = [&](bool first, bool last) {
         int at = tid;
         asm volatile("" : "+v"(at));
         const int l15 = at & 15, l4 = (at >> 4 & 3) * 4;
@@ -260,10 +262,12 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
 #pragma unroll
             for (int y = 0; y < TJ; ++y) {
                 const int ti = wi + 16 * x + (YROWS ? l15 : l4), tj = wj + 16 * y + (YROWS ? l4 : l15);
-                if (part)
-                    *reinterpret_cast<f32x4_t*>(part + (YROWS ? ti * BJ + tj : tj * BI + ti)) = acc[x][y];
+                f32x4_t* so_far = reinterpret_cast<f32x4_t*>(sums + (YROWS ? ti * BJ + tj : tj * BI + ti));
+                if (!first) acc[x][y] += *so_far;
+                if (whole && last)
+                    store_four<YROWS>(a, n, i0 + ti, j0 + tj, acc[x][y]);
                 else
-                    store_four<YROWS>(a, n, i0 + ti, j0 + tj, acc[x][y], first);
+                    *so_far = acc[x][y];
                 acc[x][y] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
     };
@@ -275,7 +279,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
         stage();
     }
     for (bool first = true;; first = false) {
-        const int64_t end = g.flush && !part ? lesser(t + g.flush, t1) : t1;
+        const int64_t end = g.flush && whole ? lesser(t + g.flush, t1) : t1;
         for (; t < end; ++t) {
             __syncthreads();
             if (t + 1 < t1) fetch();
@@ -283,7 +287,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
             __syncthreads();
             if (t + 1 < t1) stage();
         }
-        put(first);
+        put(first, t >= t1);
         if (t >= t1) break;
     }
 }
@@ -359,13 +363,14 @@ Plan make_plan(const MxArgs& a, bool x) {
     p.by_columns = bf16 && !a.x_rows && a.ldx % 2 == 0 && a.ldx < (int64_t(1) << 31) / 128 && at % 4 == 0;
     p.pack = !p.by_columns && !(bf16 && a.x_rows && terms % kStep == 0 && a.ldx % 8 == 0 && at % 16 == 0);
     p.pack_bytes = round_up(p.planes * p.plane * 2, 256);
-    p.cut = cut_tiles(a.s, n, p.steps * p.planes);
+    p.cut = cut_tiles(a.s, n, p.steps * p.planes, kChain / kStep);
     return p;
 }
 
 template <int BITS, bool TRANS, bool PT>
-hipError_t launch_tiles(const MxArgs& a, const TileArgs& g, bool large, hipStream_t st) {
-    const dim3 grid(static_cast<uint32_t>(g.cut.groups()));
+hipError_t launch_tiles(const MxArgs& a, const TileArgs& g, int64_t groups, hipStream_t st) {
+    const bool large = g.cut.large;
+    const dim3 grid(static_cast<uint32_t>(groups));
     const auto kernel = large ? (a.y_rows ? mx_tile_kernel<BITS, TRANS, PT, 4, 8, true> : mx_tile_kernel<BITS, TRANS, PT, 4, 8, false>)
                               : (a.y_rows ? mx_tile_kernel<BITS, TRANS, PT, 2, 4, true> : mx_tile_kernel<BITS, TRANS, PT, 2, 4, false>);
     kernel<<<grid, kThreads, 0, st>>>(a, g);
@@ -373,9 +378,9 @@ hipError_t launch_tiles(const MxArgs& a, const TileArgs& g, bool large, hipStrea
 }
 
 template <int BITS>
-hipError_t launch_bits(const MxArgs& a, const TileArgs& g, const Plan& p, hipStream_t st) {
-    if (a.trans) return p.by_columns ? launch_tiles<BITS, true, true>(a, g, p.cut.large, st) : launch_tiles<BITS, true, false>(a, g, p.cut.large, st);
-    return p.by_columns ? launch_tiles<BITS, false, true>(a, g, p.cut.large, st) : launch_tiles<BITS, false, false>(a, g, p.cut.large, st);
+hipError_t launch_bits(const MxArgs& a, const TileArgs& g, const Plan& p, int64_t groups, hipStream_t st) {
+    if (a.trans) return p.by_columns ? launch_tiles<BITS, true, true>(a, g, groups, st) : launch_tiles<BITS, true, false>(a, g, groups, st);
+    return p.by_columns ? launch_tiles<BITS, false, true>(a, g, groups, st) : launch_tiles<BITS, false, false>(a, g, groups, st);
 }
 
 }  // namespace
@@ -391,7 +396,7 @@ bool mx_tiled_serves(const MxArgs& a) {
 
 int64_t mx_tiled_workspace_bytes(const MxArgs& a) {
     const Plan p = make_plan(a, false);
-    return p.pack_bytes + p.cut.part_bytes();
+    return p.pack_bytes + p.cut.sums_bytes();
 }
 
 hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
@@ -405,8 +410,8 @@ hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
     g.planes = p.planes;
     g.steps = p.steps;
     g.cut = p.cut;
-    g.part = p.cut.splits > 1 ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + p.pack_bytes) : nullptr;
-    g.flush = a.y_bf16 ? 0 : 16384 / kStep;
+    g.sums = p.cut.sums_bytes() ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + p.pack_bytes) : nullptr;
+    g.flush = a.y_bf16 ? 0 : kChain / kStep;
     if (!grid_fits(p.cut.groups(), kThreads)) return hipErrorInvalidConfiguration;
     if (a.x_bits && p.pitch > 0) {
         const int64_t blocks = ceil_div(a.s * (p.pitch / 8), 256);
@@ -423,9 +428,12 @@ hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const hipError_t e = a.A.bits == 4 ? launch_bits<4>(a, g, p, st) : launch_bits<8>(a, g, p, st);
-    if (e != hipSuccess || !g.part) return e;
-    return launch_shared_tiles(a, p.cut, g.part, n, st);
+    const hipError_t e = over_groups(p.cut, [&](int64_t first, int64_t groups) {
+        g.first = first;
+        return a.A.bits == 4 ? launch_bits<4>(a, g, p, groups, st) : launch_bits<8>(a, g, p, groups, st);
+    });
+    if (e != hipSuccess || p.cut.splits <= 1) return e;
+    return launch_shared_tiles(a, p.cut, g.sums, n, st);
 }
 
 }  // namespace coded

@@ -651,3 +651,61 @@ def test_microscaled_rows_of_x_eight_megabytes_apart(lib, torch, bits, x_bits, f
         lib.coded_mx_mm(M, X, Y, x_rows=True, y_rows=y_rows)
         want = A @ X64.t()
         assert torch.equal(Y.double(), want.t() if y_rows else want)
+
+
+def dense_whole(torch, x, s, k, x_rows, g):
+    """(X, its values s x k in 64 bits): whole numbers up to 7, or 4-bit codes of them (rows)."""
+    if x == "mx4":
+        c, e, v = whole_codes(torch, s, k, g)
+        return (c, e), v
+    X = torch.randint(-7, 8, (s, k) if x_rows else (k, s), device="cuda", generator=g).to(torch.float32 if x == "f32" else torch.bfloat16)
+    return X, X.double() if x_rows else X.double().t()
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("x", ["f32", "bf16", "mx4"])
+@pytest.mark.parametrize("n,k,s", [(8192, 16500, 2048), (8200, 33000, 2100), (520, 66000, 260)])
+def test_long_sums_are_rounded_once_after_alpha_and_c(lib, torch, transposed, x, n, k, s):
+    """Sums that are exact in fp32, of more than one chain, and a C that is far larger: alpha S + beta C in fp32 has one
+    right answer.  C apart from Y, in Y itself, and as one row."""
+    if transposed and x == "mx4":
+        pytest.skip("U is dense")
+    g = torch.Generator(device="cuda").manual_seed(n + k)
+    q, r = (k, n) if transposed else (n, k)
+    codes, scales, A = whole_codes(torch, q, r, g)
+    M = lib.MXMatrix(codes, scales, r, lib.CODED_MX4)
+    A = A.t() if transposed else A
+    call = lib.coded_mx_mm_t if transposed else lib.coded_mx_mm
+    X, X64 = dense_whole(torch, x, s, k, True, g)
+    if x == "mx4":
+        X = lib.MXMatrix(*X, k, lib.CODED_MX4)
+    S = X64 @ A.t()
+    del A, X64
+    assert float(S.abs().max()) < 2 ** 23
+    for y_rows in (True, False):
+        want = S if y_rows else S.t()
+        C = (torch.randint(-100, 101, want.shape, device="cuda", generator=g) * 2.0 ** 24 + 2.0 ** 20).float()
+        Y = C.clone()
+        call(M, X, Y, x_rows=True, y_rows=y_rows, alpha=-0.5, beta=1.0, C=Y)
+        assert torch.equal(Y, (C.double() - 0.5 * want).float())
+        call(M, X, Y, x_rows=True, y_rows=y_rows, alpha=2.0, beta=-1.0, C=C)
+        assert torch.equal(Y, (2.0 * want - C.double()).float())
+        call(M, X, Y, x_rows=True, y_rows=y_rows, alpha=1.0, beta=1.0, C=C[5])
+        assert torch.equal(Y, (want + C[5].double()).float())
+
+
+@pytest.mark.parametrize("transposed,x,n,k,s", [(False, "f32", 16385, 5500, 10100), (True, "f32", 16385, 5500, 10100), (False, "mx4", 16385, 16500, 10100)])
+def test_more_tiles_of_long_sums_than_one_launch_takes(lib, torch, transposed, x, n, k, s):
+    g = torch.Generator(device="cuda").manual_seed(16)
+    q, r = (k, n) if transposed else (n, k)
+    codes, scales, A = whole_codes(torch, q, r, g)
+    M = lib.MXMatrix(codes, scales, r, lib.CODED_MX4)
+    A = A.t() if transposed else A
+    X, X64 = dense_whole(torch, x, s, k, True, g)
+    if x == "mx4":
+        X = lib.MXMatrix(*X, k, lib.CODED_MX4)
+    Y = torch.empty((s, n), device="cuda")
+    (lib.coded_mx_mm_t if transposed else lib.coded_mx_mm)(M, X, Y, x_rows=True, y_rows=True)
+    S = X64 @ A.t()
+    assert float(S.abs().max()) < 2 ** 24
+    assert torch.equal(Y.double(), S)
