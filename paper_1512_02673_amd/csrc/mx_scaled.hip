@@ -28,7 +28,7 @@ struct ScaledArgs {
     Cut cut;
     int64_t first;   // these three as in mx_tiled.hip
     float* sums;
-    int32_t flush;
+    int64_t chain;
 };
 
 // The rows of codes and scales that one side of a tile takes of a step.
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_scaled_kernel(MxArgs a, Scaled
         stage();
     }
     for (bool first = true;; first = false) {
-        const int64_t end = g.flush && whole ? lesser(t + g.flush, t1) : t1;
+        const int64_t end = lesser(t + g.chain, t1);
         for (; t < end; ++t) {
             __syncthreads();
             if (t + 1 < t1) fetch(t + 1);
@@ -185,7 +185,7 @@ hipError_t launch_mx_scaled(const MxArgs& a, hipStream_t st) {
     g.steps = ceil_div(a.r, kStep);
     g.cut = c;
     g.sums = static_cast<float*>(a.workspace);
-    g.flush = a.y_bf16 ? 0 : kChain / kStep;
+    g.chain = chain_steps(a, kStep);
     if (!grid_fits(c.groups(), kThreads)) return hipErrorInvalidConfiguration;
     const auto kernel = c.large ? (a.y_rows ? mx_scaled_kernel<4, 8, true> : mx_scaled_kernel<4, 8, false>)
                                 : (a.y_rows ? mx_scaled_kernel<2, 4, true> : mx_scaled_kernel<2, 4, false>);

@@ -10,7 +10,11 @@ namespace coded {
 namespace {
 
 constexpr int kThreads = 256;   // of a tile's workgroup: two waves along each of its sides
-constexpr int kChain = 16384;   // terms added up in registers before the sums move to memory
+// Terms added up in registers before the sums move to memory, 32 or 128 an addition.  Next to the magnitudes, 512
+// roundings of 2^-24 are 2^-15; a bf16 result is rounded to 2^-9, and 2048 of them, 2^-13, are a sixteenth of that.
+// (8192 x 33000 times 4096 tokens, bf16 results: 2.21 ms with the short chain, 2.14 with the long one and without.)
+constexpr int kChain = 16384, kChainBf16 = 65536;
+inline int64_t chain_steps(const MxArgs& a, int step) { return (a.y_bf16 ? kChainBf16 : kChain) / step; }
 // How many right-hand sides and results a tile has, and which tiles' sums are shared by several workgroups: the
 // first `whole` tiles are one workgroup's each, the rest are split along the terms.
 struct Cut {
@@ -39,7 +43,7 @@ inline double step_us(bool large, int64_t groups) {
 // 16, and small ones): 512 x 4096 of 4096 terms 86 57 41 46 68, 47 41 42 52 70 us; 578 x 6075 of 71240 terms in
 // three planes 4321 2249 1874 1885 1892, 3043 3186 3323 3249 2682; 1000 x 1000 of 16384 terms 307 166 92 63 62,
 // 163 95 67 68 72.
-// `chain`: steps of a chain.
+// `chain`: steps of the shorter chain (the workspace is asked for without the results' type).
 inline Cut cut_tiles(int64_t s, int64_t n, int64_t steps, int64_t chain) {
     Cut best{};
     double best_us = -1;

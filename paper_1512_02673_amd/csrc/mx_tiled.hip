@@ -41,7 +41,7 @@ struct TileArgs {
     Cut cut;
     int64_t first;              // workgroup of this launch among all
     float* sums;                // whole tiles' sums of the chains so far, then those of the shared tiles' splits
-    int32_t flush;              // steps summed in one chain (fp32 results), 0: all
+    int64_t chain;              // steps of a chain
 };
 
 // Two waves along each side of the tile, each of TI x TJ tiles of 16 x 16.
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
         stage();
     }
     for (bool first = true;; first = false) {
-        const int64_t end = g.flush && whole ? lesser(t + g.flush, t1) : t1;
+        const int64_t end = lesser(t + g.chain, t1);
         for (; t < end; ++t) {
             __syncthreads();
             if (t + 1 < t1) fetch();
@@ -411,7 +411,7 @@ hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
     g.steps = p.steps;
     g.cut = p.cut;
     g.sums = p.cut.sums_bytes() ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + p.pack_bytes) : nullptr;
-    g.flush = a.y_bf16 ? 0 : kChain / kStep;
+    g.chain = chain_steps(a, kStep);
     if (!grid_fits(p.cut.groups(), kThreads)) return hipErrorInvalidConfiguration;
     if (a.x_bits && p.pitch > 0) {
         const int64_t blocks = ceil_div(a.s * (p.pitch / 8), 256);

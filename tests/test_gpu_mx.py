@@ -709,3 +709,43 @@ def test_more_tiles_of_long_sums_than_one_launch_takes(lib, torch, transposed, x
     S = X64 @ A.t()
     assert float(S.abs().max()) < 2 ** 24
     assert torch.equal(Y.double(), S)
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("x", ["f32", "bf16", "mx4"])
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+@pytest.mark.parametrize("s", [512, 2048])
+def test_small_terms_beside_a_large_one_are_lost_to_one_chain_at_most(lib, torch, transposed, x, y, s):
+    """Sums of 2^24, 31 zeros and k - 32 terms of 2^-6, by splits of tiles and by whole ones.  Next to 2^24 (fp32
+    numbers there are 2 apart) the small terms may go missing, but those of the large term's chain alone, 16384 (bf16
+    results: 65536): every other chain is exact, and adding up the chains' and splits' sums, at most 64 + k / 16384 of
+    them, loses up to 2 each."""
+    if transposed and x == "mx4":
+        pytest.skip("U is dense")
+    n, k = 8192, 262144
+    q, r = (k, n) if transposed else (n, k)
+    sign = torch.where(torch.arange(n, device="cuda") % 3 == 0, -1.0, 1.0)
+    nibble = torch.where(sign < 0, 0xA, 0x2).to(torch.uint8)   # -1, 1
+    if transposed:
+        codes = (nibble[0::2] | nibble[1::2] << 4).repeat(q, 1)
+    else:
+        codes = (nibble | nibble << 4)[:, None].repeat(1, r // 2)
+    M = lib.MXMatrix(codes, torch.full((q, r // 32), 127, dtype=torch.uint8, device="cuda"), r, lib.CODED_MX4)
+    if x == "mx4":
+        xc = torch.full((s, k // 2), 0x22, dtype=torch.uint8, device="cuda")
+        xc[:, 1:16] = 0
+        xc[:, 0] = 2
+        xs = torch.full((s, k // 32), 127 - 6, dtype=torch.uint8, device="cuda")
+        xs[:, 0] = 127 + 24
+        X = lib.MXMatrix(xc, xs, k, lib.CODED_MX4)
+    else:
+        X = torch.full((s, k), 2.0 ** -6, dtype=torch.float32 if x == "f32" else torch.bfloat16, device="cuda")
+        X[:, 1:32] = 0
+        X[:, 0] = 2.0 ** 24
+    C = (-2.0 ** 24 * sign).to(torch.bfloat16 if y == "bf16" else torch.float32)
+    Y = torch.empty((s, n), dtype=C.dtype, device="cuda")
+    (lib.coded_mx_mm_t if transposed else lib.coded_mx_mm)(M, X, Y, x_rows=True, y_rows=True, beta=1.0, C=C)
+    want = (k - 32) * 2.0 ** -6
+    bound = (65536 if y == "bf16" else 16384) * 2.0 ** -6 + 2 * (64 + k / 16384) + (2.0 ** -8 * want if y == "bf16" else 0)
+    worst = float((Y.double() * sign - want).abs().max())
+    assert worst <= bound, (worst, bound)
