@@ -545,6 +545,7 @@ coded_status coded_mx_workspace(int32_t transposed, coded_dtype fmt, int64_t q, 
  *   y_dt      CODED_F32 or CODED_BF16.  Products are exact, sums are in fp32
  *             (an fp32 X enters with all its bits); alpha and beta C meet the
  *             whole sum, in fp32, and the result of that is rounded to y_dt.
+ *   alpha     enters in fp32, as beta does; finite there.
  *   C         of y_dt, in Y's order with row stride ldcc (0: one row that every
  *             row of Y gets, a bias); may be Y itself.  Not read, and may be
  *             NULL, when beta == 0.

@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 #include <exception>
+#include <limits>
 #include <new>
 
 #include "mx.h"
@@ -89,7 +90,10 @@ coded_status product(bool trans, coded_dtype fmt, const void* codes, int64_t ldc
     const int64_t rows = a.y_rows ? s : n, cols = a.y_rows ? n : s;
     st = check_dense("Y", y_dt, Y, rows, cols, ldy);
     if (st != CODED_OK) return st;
-    if (!std::isfinite(alpha) || !std::isfinite(beta)) return fail(CODED_ERR_ARG, "alpha and beta must be finite");
+    const double top = std::numeric_limits<float>::max();   // they enter in fp32
+    if (!(std::fabs(alpha) <= top && std::fabs(beta) <= top)) return fail(CODED_ERR_ARG, "alpha and beta must be finite in fp32");
+    a.alpha = static_cast<float>(alpha);
+    a.beta = static_cast<float>(beta);
     if (beta != 0.0) {
         // a row stride of 0 gives every row of Y the same row of C
         st = check_dense("C", y_dt, C, rows, cols, ldcc == 0 ? std::max<int64_t>(cols, 1) : ldcc);
@@ -101,8 +105,6 @@ coded_status product(bool trans, coded_dtype fmt, const void* codes, int64_t ldc
     a.Y = Y;
     a.ldy = ldy;
     a.y_bf16 = y_dt == CODED_BF16;
-    a.alpha = static_cast<float>(alpha);
-    a.beta = static_cast<float>(beta);
     if (n == 0 || s == 0) return CODED_OK;
     const int64_t need = mx_workspace_bytes(a);
     if (need > 0) {

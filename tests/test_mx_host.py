@@ -215,3 +215,17 @@ def test_workspace_of_a_call_on_a_stream_is_that_streams(lib, monkeypatch, trans
     monkeypatch.setattr(lib, "lib", Library)
     (lib.coded_mx_mm_t if transposed else lib.coded_mx_mm)(M, X, Y, stream=side)
     assert fake.asked == [side] and fake.current is None
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("change", [dict(alpha=1e300), dict(alpha=-3.5e38), dict(beta=1e39, C=0x5000, ldcc=2), dict(beta=-1e300, C=0x5000, ldcc=2)])
+def test_alpha_and_beta_that_are_no_fp32_numbers_are_refused(lib, transposed, change):
+    """They enter in fp32, where these would be infinite."""
+    assert _call(lib, transposed, **change) == lib.CODED_ERR_ARG
+    assert "alpha and beta" in lib.last_error()
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+def test_alpha_and_beta_of_the_largest_fp32_number_pass(lib, transposed):
+    top = float(np.finfo(np.float32).max)
+    assert _call(lib, transposed, s=0, alpha=top, beta=-top, C=0x5000, ldcc=2) == lib.CODED_OK
