@@ -23,6 +23,8 @@ coded_status guarded(F f) {
 
 bool aligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
+constexpr int64_t kMostSize = int64_t(1) << 40;
+
 int bits_of(coded_dtype fmt) { return fmt == CODED_MX4 ? 4 : fmt == CODED_MX8 ? 8 : 0; }
 
 int64_t code_pitch(int bits, int64_t r) { return ceil_div(r, kMxBlock) * kMxBlock / 8 * bits; }
@@ -35,7 +37,7 @@ coded_status check_mx(const char* name, coded_dtype fmt, const void* codes, int6
     const int bits = bits_of(fmt);
     if (!bits) return fail(CODED_ERR_ARG, what + ": the format must be CODED_MX4 or CODED_MX8");
     if (rows < 0 || cols < 0) return fail(CODED_ERR_SHAPE, what + ": sizes must be >= 0");
-    if (cols > (int64_t(1) << 40) || rows > (int64_t(1) << 40)) return fail(CODED_ERR_SHAPE, what + ": sizes must be <= 2^40");
+    if (cols > kMostSize || rows > kMostSize) return fail(CODED_ERR_SHAPE, what + ": sizes must be <= 2^40");
     if (ldc < code_pitch(bits, cols) || ldc % 16 != 0)
         return fail(CODED_ERR_SHAPE, what + ": the code pitch must be a multiple of 16 bytes that holds a row");
     if (lds < scale_pitch(cols) || lds % 4 != 0)
@@ -67,7 +69,7 @@ coded_status product(bool trans, coded_dtype fmt, const void* codes, int64_t ldc
     MxArgs a{};
     coded_status st = check_mx("A", fmt, codes, ldc, scales, lds, q, r, a.A);
     if (st != CODED_OK) return st;
-    if (s < 0 || s > (int64_t(1) << 40)) return fail(CODED_ERR_SHAPE, "s must be in [0, 2^40]");
+    if (s < 0 || s > kMostSize) return fail(CODED_ERR_SHAPE, "s must be in [0, 2^40]");
     if (order & ~(CODED_X_ROWS | CODED_Y_ROWS)) return fail(CODED_ERR_ARG, "order has unknown bits");
     a.q = q;
     a.r = r;
@@ -129,7 +131,7 @@ coded_status coded_mx_sizes(coded_dtype fmt, int64_t r, int64_t* code_pitch_out,
     return guarded([&] {
         const int bits = bits_of(fmt);
         if (!bits) return fail(CODED_ERR_ARG, "the format must be CODED_MX4 or CODED_MX8");
-        if (r < 0 || r > (int64_t(1) << 40)) return fail(CODED_ERR_SHAPE, "r must be in [0, 2^40]");
+        if (r < 0 || r > kMostSize) return fail(CODED_ERR_SHAPE, "r must be in [0, 2^40]");
         if (code_pitch_out) *code_pitch_out = code_pitch(bits, r);
         if (scale_pitch_out) *scale_pitch_out = scale_pitch(r);
         return CODED_OK;
@@ -143,7 +145,7 @@ coded_status coded_mx_workspace(int32_t transposed, coded_dtype fmt, int64_t q, 
         if (!bits_of(fmt)) return fail(CODED_ERR_ARG, "the format must be CODED_MX4 or CODED_MX8");
         if (x_dt != CODED_F32 && x_dt != CODED_BF16 && (transposed || !bits_of(x_dt)))
             return fail(CODED_ERR_ARG, "x_dt is not a type of X");
-        if (q < 0 || r < 0 || s < 0) return fail(CODED_ERR_SHAPE, "sizes must be >= 0");
+        if (q < 0 || r < 0 || s < 0 || std::max(std::max(q, r), s) > kMostSize) return fail(CODED_ERR_SHAPE, "sizes must be in [0, 2^40]");
         if (order & ~(CODED_X_ROWS | CODED_Y_ROWS)) return fail(CODED_ERR_ARG, "order has unknown bits");
         MxArgs a{};
         a.A.bits = bits_of(fmt);

@@ -229,3 +229,12 @@ def test_alpha_and_beta_that_are_no_fp32_numbers_are_refused(lib, transposed, ch
 def test_alpha_and_beta_of_the_largest_fp32_number_pass(lib, transposed):
     top = float(np.finfo(np.float32).max)
     assert _call(lib, transposed, s=0, alpha=top, beta=-top, C=0x5000, ldcc=2) == lib.CODED_OK
+
+
+@pytest.mark.parametrize("sizes", [(2 ** 41, 64, 1), (64, 2 ** 41, 1), (64, 64, 2 ** 41), (64, 64, 2 ** 62), (2 ** 62, 2 ** 62, 2 ** 62)])
+@pytest.mark.parametrize("transposed", [0, 1])
+def test_workspace_of_sizes_that_no_call_takes_is_refused(lib, transposed, sizes):
+    b = ctypes.c_int64()
+    q, r, s = sizes
+    assert lib.lib().coded_mx_workspace(transposed, 3, q, r, 0, s, 0, ctypes.addressof(b)) == lib.CODED_ERR_SHAPE
+    assert lib.last_error()
