@@ -1,9 +1,9 @@
 // Which kernel a product with a microscaled matrix takes, and the general one.
 //
 // The general kernel takes every size and stride: it is for matrices whose rows
-// are 8 MB and more apart, where the others' 32-bit offsets within a tile's rows
-// do not reach (2 x 16777221, two columns: 0.75 s, one workgroup walking down the
-// rows).  Each element comes by itself, so nothing is aligned or bounded.
+// are 8 MB and more apart (A's, or a 4-bit X's that meets a 4-bit A), where the
+// others' 32-bit offsets within a tile's rows do not reach (2 x 16777221, two
+// columns: 0.75 s, one workgroup walking down the rows).  Each element comes by itself, so nothing is aligned or bounded.
 //
 // A code times its scale is a bf16 value, exactly, and so is each of the three
 // pieces of an fp32 X, so the matrix cores' bf16 products are exact in fp32 and

@@ -4,10 +4,11 @@
 //
 // P is X in bf16.  X is taken as it is where a row holds whole steps of a right-hand
 // side, 16-byte aligned, or where a row holds one term of all of them (by columns);
-// else it goes through the workspace: unpacked from codes, which is exact, or copied
-// with k contiguous and padded with zeros, an fp32 X as three planes (split_bf16)
-// whose products are summed one after the other.  Terms past the last one are zeros
-// on one side and finite on the other; rows past the end of A read as zeros.
+// else it goes through the workspace: unpacked from codes, which is exact, or copied,
+// an fp32 X as three planes (split_bf16) whose products are summed one after the
+// other.  There each step's 64 terms of all sides lie together, a side's contiguous
+// and padded with zeros, so that no offset within a step grows with the terms.  Terms
+// past the last one are zeros on one side and finite on the other; rows past the end of A read as zeros.
 //
 // Bound: the matrix cores, and the power they take: they were busy half of the
 // cycles at about 2.1 GHz (operands of zeros instead of data: 10 to 18% faster, a
@@ -34,8 +35,8 @@ constexpr int kStep = 64;   // terms
 
 struct TileArgs {
     const uint16_t* P;
-    int64_t pitch, plane;       // elements between rows, and between planes
-    int64_t row;                // elements of a row that are there: whole steps (by columns: rows)
+    int64_t pitch, step, plane; // elements between rows of a step, between steps, and between planes
+    int64_t extent;             // elements from the first to the last of a plane
     int32_t planes;
     int64_t steps;              // of one plane
     Cut cut;
@@ -93,11 +94,10 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     const int64_t q_skip = TRANS ? j0 * BITS / 8 : j0 * a.A.ldc, s_skip = TRANS ? j0 / kMxBlock : j0 * a.A.lds;
     const int64_t q_all = (a.q - 1) * a.A.ldc + code_row - q_skip;
     const int64_t s_all = (a.q - 1) * a.A.lds + (TRANS ? blocks : ceil_div(blocks, 4) * 4) - s_skip;
-    const int64_t plane = t0 > 0 ? t0 / g.steps : 0, p_step = PT ? kStep * g.pitch : kStep;
+    const int64_t plane = t0 > 0 ? t0 / g.steps : 0, p_step = g.step;
     const uint16_t* p_base = g.P + plane * g.plane + (PT ? i0 : i0 * g.pitch) + step * p_step;
-    // By columns the bound is a whole number of words, as loads are: with an odd number of sides the last word holds the
-    // last side and one element more, which belongs to no side (rows start at words, so it is in the last row's word).
-    const int64_t p_all = PT ? ((g.row - 1) * g.pitch + a.s - i0 + 1) / 2 * 2 : (a.s - i0 - 1) * g.pitch + g.row;
+    // by columns the extent is a whole number of words, as loads are: see launch_mx_tiled
+    const int64_t p_all = g.extent - (PT ? i0 : i0 * g.pitch);
     int64_t p_left = (p_all - step * p_step) * 2;
     const uint8_t *q_base = a.A.codes + q_skip + step * q_step, *s_base = a.A.scales + s_skip + step * s_step;
     int64_t q_left = q_all - step * q_step, s_left = s_all - step * s_step;
@@ -292,10 +292,13 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     }
 }
 
-// A microscaled X in bf16 (exact), k contiguous: to[side][pitch], zeros from `terms` on.  A thread takes eight values.
-__global__ __launch_bounds__(256) void mx_unpack_kernel(MxMat x, int64_t s, int64_t terms, uint16_t* to, int64_t pitch) {
-    const int64_t id = blockIdx.x * int64_t(256) + threadIdx.x, per = pitch / 8;
-    const int64_t side = id / per, k = id % per * 8;
+// A side's eight terms from k on, among steps of all sides (a plane of the workspace).
+__device__ __forceinline__ int64_t packed_at(int64_t side, int64_t k, int64_t s) { return (k / kStep * s + side) * kStep + k % kStep; }
+
+// A microscaled X in bf16 (exact), zeros from `terms` on.  A thread takes eight values.
+__global__ __launch_bounds__(256) void mx_unpack_kernel(MxMat x, int64_t s, int64_t terms, uint16_t* to, int64_t pieces) {
+    const int64_t id = blockIdx.x * int64_t(256) + threadIdx.x;
+    const int64_t side = id / pieces, k = id % pieces * 8;
     if (side >= s) return;
     uint32_t v[4] = {0u, 0u, 0u, 0u};
     if (k < terms) {   // up to the end of its last block a row's codes are zero
@@ -304,17 +307,16 @@ __global__ __launch_bounds__(256) void mx_unpack_kernel(MxMat x, int64_t s, int6
         else
             mx_eight<8>(x.codes + side * x.ldc, x.scales + side * x.lds, k, v);
     }
-    *reinterpret_cast<u32x4_t*>(to + side * pitch + k) = u32x4_t{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<u32x4_t*>(to + packed_at(side, k, s)) = u32x4_t{v[0], v[1], v[2], v[3]};
 }
 
-// X in bf16, k contiguous: to[plane][side][pitch], zeros from `terms` on.  A workgroup takes 64 sides x 64 terms.
+// X in bf16, zeros from `terms` on.  A workgroup takes 64 sides of a step.
 template <bool BF16>
 __global__ __launch_bounds__(256) void mx_pack_kernel(const void* X, int64_t ldx, int32_t x_rows, int64_t s, int64_t terms, uint16_t* to,
-                                                      int64_t pitch, int64_t plane) {
+                                                      int64_t steps, int64_t plane) {
     constexpr int PL = BF16 ? 1 : 3;
     __shared__ uint16_t tile[PL][64][66];
-    const int64_t strips = ceil_div(pitch, 64);
-    const int64_t k0 = blockIdx.x % strips * 64, i0 = blockIdx.x / strips * 64;
+    const int64_t k0 = blockIdx.x % steps * kStep, i0 = blockIdx.x / steps * 64;
     const int lo = threadIdx.x & 63, hi = threadIdx.x >> 6;
     for (int e = 0; e < 16; ++e) {
         // consecutive threads on consecutive elements of X
@@ -333,10 +335,10 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const void* X, int64_t ldx
     }
     __syncthreads();
     for (int e = 0; e < 16; ++e) {
-        const int64_t i = i0 + hi + 4 * e, k = k0 + lo;
-        if (i < s && k < pitch)
+        const int64_t i = i0 + hi + 4 * e;
+        if (i < s)
 #pragma unroll
-            for (int h = 0; h < PL; ++h) to[h * plane + i * pitch + k] = tile[h][hi + 4 * e][lo];
+            for (int h = 0; h < PL; ++h) to[h * plane + packed_at(i, k0 + lo, s)] = tile[h][hi + 4 * e][lo];
     }
 }
 
@@ -344,7 +346,7 @@ __global__ __launch_bounds__(256) void mx_pack_kernel(const void* X, int64_t ldx
 struct Plan {
     bool pack, by_columns;   // X goes through the workspace; it is taken as it is, a term of every side a row
     int planes;
-    int64_t steps, pitch, plane, pack_bytes;
+    int64_t steps, plane, pack_bytes;
     Cut cut;
 };
 
@@ -356,12 +358,12 @@ Plan make_plan(const MxArgs& a, bool x) {
     const int64_t terms = a.trans ? a.q : a.r, n = a.trans ? a.r : a.q;
     p.planes = a.x_bits || a.x_bf16 ? 1 : 3;
     p.steps = ceil_div(terms, kStep);
-    p.pitch = p.steps * kStep;
-    p.plane = a.s * p.pitch;
+    p.plane = a.s * p.steps * kStep;
     const uintptr_t at = reinterpret_cast<uintptr_t>(a.X);
     const bool bf16 = x && !a.x_bits && a.x_bf16;
-    p.by_columns = bf16 && !a.x_rows && a.ldx % 2 == 0 && a.ldx < (int64_t(1) << 31) / 128 && at % 4 == 0;
-    p.pack = !p.by_columns && !(bf16 && a.x_rows && terms % kStep == 0 && a.ldx % 8 == 0 && at % 16 == 0);
+    const bool near = a.ldx < (int64_t(1) << 31) / 256;   // offsets within a tile's rows are 32-bit
+    p.by_columns = bf16 && !a.x_rows && near && a.ldx % 2 == 0 && at % 4 == 0;
+    p.pack = !p.by_columns && !(bf16 && a.x_rows && near && terms % kStep == 0 && a.ldx % 8 == 0 && at % 16 == 0);
     p.pack_bytes = round_up(p.planes * p.plane * 2, 256);
     p.cut = cut_tiles(a.s, n, p.steps * p.planes, kChain / kStep);
     return p;
@@ -385,13 +387,12 @@ hipError_t launch_bits(const MxArgs& a, const TileArgs& g, const Plan& p, int64_
 
 }  // namespace
 
-// Offsets within a tile's rows, of X and of codes, are 32-bit.  Two 4-bit matrices with rows of X further apart than
+// Offsets within a tile's rows of codes are 32-bit.  Two 4-bit matrices with rows of X further apart than
 // mx_scaled_kernel takes go to the general kernel: the workspace is asked for by sizes, and by those that product
 // has none for an X in bf16.
 bool mx_tiled_serves(const MxArgs& a) {
     const int64_t most = (int64_t(1) << 31) / 256;
-    if (a.x_bits == 4 && a.A.bits == 4) return false;
-    return (a.trans ? a.q : a.r) < most / 2 && std::max(a.A.ldc, a.A.lds) < most && (!a.x_rows || a.ldx < most / 2);
+    return !(a.x_bits == 4 && a.A.bits == 4) && std::max(a.A.ldc, a.A.lds) < most;
 }
 
 int64_t mx_tiled_workspace_bytes(const MxArgs& a) {
@@ -404,27 +405,40 @@ hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
     const int64_t n = a.trans ? a.r : a.q, terms = a.trans ? a.q : a.r;
     TileArgs g{};
     g.P = p.pack ? static_cast<const uint16_t*>(a.workspace) : static_cast<const uint16_t*>(a.X);
-    g.pitch = p.pack ? p.pitch : a.ldx;
+    if (p.pack) {
+        g.pitch = kStep;
+        g.step = a.s * kStep;
+        g.extent = p.plane;
+    } else if (p.by_columns) {
+        // With an odd number of sides the last word holds the last side and one element more, which belongs to no
+        // side (rows start at words, so it is in the last row's word).
+        g.pitch = a.ldx;
+        g.step = kStep * a.ldx;
+        g.extent = ((terms - 1) * a.ldx + a.s + 1) / 2 * 2;
+    } else {
+        g.pitch = a.ldx;
+        g.step = kStep;
+        g.extent = (a.s - 1) * a.ldx + terms;
+    }
     g.plane = p.plane;
-    g.row = p.by_columns ? terms : p.pitch;
     g.planes = p.planes;
     g.steps = p.steps;
     g.cut = p.cut;
     g.sums = p.cut.sums_bytes() ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + p.pack_bytes) : nullptr;
     g.chain = chain_steps(a, kStep);
     if (!grid_fits(p.cut.groups(), kThreads)) return hipErrorInvalidConfiguration;
-    if (a.x_bits && p.pitch > 0) {
-        const int64_t blocks = ceil_div(a.s * (p.pitch / 8), 256);
+    uint16_t* const packed = static_cast<uint16_t*>(a.workspace);
+    if (a.x_bits && p.steps > 0) {
+        const int64_t pieces = p.steps * (kStep / 8), blocks = ceil_div(a.s * pieces, 256);
         if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
-        mx_unpack_kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a.XM, a.s, terms, static_cast<uint16_t*>(a.workspace), p.pitch);
+        mx_unpack_kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a.XM, a.s, terms, packed, pieces);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-    } else if (p.pack && p.pitch > 0) {
-        const int64_t blocks = ceil_div(p.pitch, 64) * ceil_div(a.s, 64);
-        if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+    } else if (p.pack && p.steps > 0) {
         const auto kernel = a.x_bf16 ? mx_pack_kernel<true> : mx_pack_kernel<false>;
-        kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a.X, a.ldx, a.x_rows, a.s, terms,
-                                                                    static_cast<uint16_t*>(a.workspace), p.pitch, p.plane);
+        const int64_t blocks = p.steps * ceil_div(a.s, 64);
+        if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
+        kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a.X, a.ldx, a.x_rows, a.s, terms, packed, p.steps, p.plane);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -749,3 +749,26 @@ def test_small_terms_beside_a_large_one_are_lost_to_one_chain_at_most(lib, torch
     bound = (65536 if y == "bf16" else 16384) * 2.0 ** -6 + 2 * (64 + k / 16384) + (2.0 ** -8 * want if y == "bf16" else 0)
     worst = float((Y.double() * sign - want).abs().max())
     assert worst <= bound, (worst, bound)
+
+
+@pytest.mark.parametrize("transposed,x,s,x_rows,k", [(True, "bf16", 17, False, (1 << 22) + 37), (True, "bf16", 18, False, (1 << 22) + 37),
+                                                     (True, "f32", 6, False, (1 << 22) + 37), (False, "bf16", 65, False, (1 << 22) + 37),
+                                                     (False, "bf16", 65, True, (1 << 22) + 37), (False, "bf16", 65, True, (1 << 22) + 64),
+                                                     (False, "bf16", 65, True, (1 << 23) + 64), (True, "bf16", 66, True, (1 << 23) + 64)])
+def test_millions_of_terms(lib, torch, transposed, x, s, x_rows, k):
+    """More terms, and rows of X further apart, than 32-bit offsets within a tile of such rows would take."""
+    n = 40
+    q, r = (k, n) if transposed else (n, k)
+    g = torch.Generator(device="cuda").manual_seed(17)
+    codes, scales, A = whole_codes(torch, q, r, g)
+    keep = (torch.rand((q, codes.shape[1]), device="cuda", generator=g) < 0.03).to(torch.uint8)   # sums below 2^24
+    codes *= keep
+    A *= keep.repeat_interleave(2, 1)[:, :r]
+    M = lib.MXMatrix(codes, scales, r, lib.CODED_MX4)
+    A = A.t() if transposed else A
+    X, X64 = dense_whole(torch, x, s, k, x_rows, g)
+    Y = torch.empty((n, s), device="cuda")
+    (lib.coded_mx_mm_t if transposed else lib.coded_mx_mm)(M, X, Y, x_rows=x_rows)
+    want = A @ X64.t()
+    assert float((A.abs() @ X64.t().abs()).max()) < 2 ** 24
+    assert torch.equal(Y.double(), want)
