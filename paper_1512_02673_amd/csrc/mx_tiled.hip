@@ -296,8 +296,8 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
 __device__ __forceinline__ int64_t packed_at(int64_t side, int64_t k, int64_t s) { return (k / kStep * s + side) * kStep + k % kStep; }
 
 // A microscaled X in bf16 (exact), zeros from `terms` on.  A thread takes eight values.
-__global__ __launch_bounds__(256) void mx_unpack_kernel(MxMat x, int64_t s, int64_t terms, uint16_t* to, int64_t pieces) {
-    const int64_t id = blockIdx.x * int64_t(256) + threadIdx.x;
+__global__ __launch_bounds__(256) void mx_unpack_kernel(MxMat x, int64_t s, int64_t terms, uint16_t* to, int64_t pieces, int64_t first) {
+    const int64_t id = first + blockIdx.x * int64_t(256) + threadIdx.x;
     const int64_t side = id / pieces, k = id % pieces * 8;
     if (side >= s) return;
     uint32_t v[4] = {0u, 0u, 0u, 0u};
@@ -313,10 +313,10 @@ __global__ __launch_bounds__(256) void mx_unpack_kernel(MxMat x, int64_t s, int6
 // X in bf16, zeros from `terms` on.  A workgroup takes 64 sides of a step.
 template <bool BF16>
 __global__ __launch_bounds__(256) void mx_pack_kernel(const void* X, int64_t ldx, int32_t x_rows, int64_t s, int64_t terms, uint16_t* to,
-                                                      int64_t steps, int64_t plane) {
+                                                      int64_t steps, int64_t plane, int64_t first) {
     constexpr int PL = BF16 ? 1 : 3;
     __shared__ uint16_t tile[PL][64][66];
-    const int64_t k0 = blockIdx.x % steps * kStep, i0 = blockIdx.x / steps * 64;
+    const int64_t id = first + blockIdx.x, k0 = id % steps * kStep, i0 = id / steps * 64;
     const int lo = threadIdx.x & 63, hi = threadIdx.x >> 6;
     for (int e = 0; e < 16; ++e) {
         // consecutive threads on consecutive elements of X
@@ -428,19 +428,23 @@ hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
     g.chain = chain_steps(a, kStep);
     if (!grid_fits(p.cut.groups(), kThreads)) return hipErrorInvalidConfiguration;
     uint16_t* const packed = static_cast<uint16_t*>(a.workspace);
-    if (a.x_bits && p.steps > 0) {
+    constexpr int64_t kMost = int64_t(1) << 20;   // workgroups of a launch: a grid takes sixteen times as many
+    if (a.x_bits) {
         const int64_t pieces = p.steps * (kStep / 8), blocks = ceil_div(a.s * pieces, 256);
-        if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
-        mx_unpack_kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a.XM, a.s, terms, packed, pieces);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    } else if (p.pack && p.steps > 0) {
+        for (int64_t b = 0; b < blocks; b += kMost) {
+            mx_unpack_kernel<<<dim3(static_cast<uint32_t>(lesser(kMost, blocks - b))), 256, 0, st>>>(a.XM, a.s, terms, packed, pieces, b * 256);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+    } else if (p.pack) {
         const auto kernel = a.x_bf16 ? mx_pack_kernel<true> : mx_pack_kernel<false>;
         const int64_t blocks = p.steps * ceil_div(a.s, 64);
-        if (!grid_fits(blocks, 256)) return hipErrorInvalidConfiguration;
-        kernel<<<dim3(static_cast<uint32_t>(blocks)), 256, 0, st>>>(a.X, a.ldx, a.x_rows, a.s, terms, packed, p.steps, p.plane);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+        for (int64_t b = 0; b < blocks; b += kMost) {
+            kernel<<<dim3(static_cast<uint32_t>(lesser(kMost, blocks - b))), 256, 0, st>>>(a.X, a.ldx, a.x_rows, a.s, terms, packed, p.steps,
+                                                                                          p.plane, b);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
     }
     const hipError_t e = over_groups(p.cut, [&](int64_t first, int64_t groups) {
         g.first = first;

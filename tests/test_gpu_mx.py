@@ -772,3 +772,24 @@ def test_millions_of_terms(lib, torch, transposed, x, s, x_rows, k):
     want = A @ X64.t()
     assert float((A.abs() @ X64.t().abs()).max()) < 2 ** 24
     assert torch.equal(Y.double(), want)
+
+
+@pytest.mark.parametrize("x", ["bf16", "mx8"])
+def test_many_millions_of_right_hand_sides(lib, torch, x):
+    """More of X than one launch copies or unpacks."""
+    g = torch.Generator(device="cuda").manual_seed(18)
+    n, k, s = 3, 63, ((1 << 26) if x == "bf16" else (1 << 25)) + 1000
+    codes, scales, A = whole_codes(torch, n, k, g)
+    M = lib.MXMatrix(codes, scales, k, lib.CODED_MX4)
+    if x == "bf16":
+        X = torch.empty((s, k), dtype=torch.bfloat16, device="cuda").random_(-7, 8, generator=g)
+    else:
+        xc = torch.empty((s, 64), dtype=torch.uint8, device="cuda").random_(0x38, 0x40, generator=g)   # 1 to 1.875
+        xc[:, 63] = 0
+        X = lib.MXMatrix(xc, torch.full((s, 4), 127, dtype=torch.uint8, device="cuda"), k, lib.CODED_MX8)
+    Y = torch.empty((s, n), device="cuda")
+    lib.coded_mx_mm(M, X, Y, x_rows=True, y_rows=True)
+    for at in range(0, s, 1 << 22):
+        rows = slice(at, min(s, at + (1 << 22)))
+        v = X[rows].double() if x == "bf16" else torch.tensor(om.format_values(8), device="cuda")[xc[rows, :63].int()]
+        assert torch.equal(Y[rows].double(), v @ A.t()), at
