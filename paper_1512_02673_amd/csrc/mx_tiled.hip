@@ -36,7 +36,7 @@ constexpr int kStep = 64;   // terms
 struct TileArgs {
     const uint16_t* P;
     int64_t pitch, step, plane; // elements between rows of a step, between steps, and between planes
-    int64_t extent;             // elements from the first to the last of a plane
+    int64_t extent, shrink;     // elements from a step's first to the last that it may read: of the plane's first step, and fewer a step
     int32_t planes;
     int64_t steps;              // of one plane
     Cut cut;
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
     const uint16_t* p_base = g.P + plane * g.plane + (PT ? i0 : i0 * g.pitch) + step * p_step;
     // by columns the extent is a whole number of words, as loads are: see launch_mx_tiled
     const int64_t p_all = g.extent - (PT ? i0 : i0 * g.pitch);
-    int64_t p_left = (p_all - step * p_step) * 2;
+    int64_t p_left = (p_all - step * g.shrink) * 2;
     const uint8_t *q_base = a.A.codes + q_skip + step * q_step, *s_base = a.A.scales + s_skip + step * s_step;
     int64_t q_left = q_all - step * q_step, s_left = s_all - step * s_step;
     const auto fetch = [&] {
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_tile_kernel(MxArgs a, TileArgs
             }
         }
         p_base += p_step;
-        p_left -= p_step * 2;
+        p_left -= g.shrink * 2;
         q_base += q_step;
         q_left -= q_step;
         s_base += s_step;
@@ -408,16 +408,17 @@ hipError_t launch_mx_tiled(const MxArgs& a, hipStream_t st) {
     if (p.pack) {
         g.pitch = kStep;
         g.step = a.s * kStep;
-        g.extent = p.plane;
+        g.extent = a.s * kStep;   // the step's own: what a tile has beyond its sides is not read
+        g.shrink = 0;
     } else if (p.by_columns) {
         // With an odd number of sides the last word holds the last side and one element more, which belongs to no
         // side (rows start at words, so it is in the last row's word).
         g.pitch = a.ldx;
-        g.step = kStep * a.ldx;
+        g.step = g.shrink = kStep * a.ldx;
         g.extent = ((terms - 1) * a.ldx + a.s + 1) / 2 * 2;
     } else {
         g.pitch = a.ldx;
-        g.step = kStep;
+        g.step = g.shrink = kStep;
         g.extent = (a.s - 1) * a.ldx + terms;
     }
     g.plane = p.plane;
