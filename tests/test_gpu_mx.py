@@ -587,7 +587,7 @@ def test_an_odd_number_of_columns_of_x_in_even_rows(lib, torch, transposed, bits
     """bf16 columns that are read as they are: with s odd the last row's last word holds the last side's term and
     nothing else of X.  That row is made of numbers that every last side's result shows."""
     g = torch.Generator(device="cuda").manual_seed(5)
-    for n, k, s in ((300, 1, 67), (700, 300, 131), (90, 3, 67), (260, 64, 65), (8200, 130, 1101), (130, 65, 8191), (8200, 128, 1027)):
+    for n, k, s in ((300, 1, 67), (700, 300, 131), (90, 3, 67), (260, 64, 65), (8200, 130, 1101), (130, 65, 8191), (8200, 128, 1027), (8200, 130, 2047)):
         q, r = (k, n) if transposed else (n, k)
         codes, scales, A = whole_codes_of(torch, bits, q, r, g)
         M = lib.MXMatrix(codes, scales, r, fmt_of(lib, bits))
