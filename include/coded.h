@@ -499,8 +499,9 @@ coded_status coded_shuffle_decode(const float* A, int64_t q, int64_t r, int64_t 
  * coded_mx_sizes gives the smallest pitches.  A row of a matrix, or any run of
  * rows, is such a matrix at its own first row, so a block row of A is used as
  * it lies.  Products take A's values as they are: a code times its scale is a
- * bfloat16 value (scales below 2^-117, which coded_mx_quantize does not write,
- * may give values that are too small to be one).
+ * bfloat16 value (scales below 2^-117 may give values that are too small to be
+ * one, and codes whose value would be 2^128 or more are infinities;
+ * coded_mx_quantize writes neither).
  * Right-hand sides and results: columns of X (k x s, row stride ldx >= s) and of
  * Y (n x s, ldy >= s) unless `order` says that a right-hand side is a row of X
  * (CODED_X_ROWS: s x k, ldx >= k) or of Y (CODED_Y_ROWS: s x n, ldy >= n), as

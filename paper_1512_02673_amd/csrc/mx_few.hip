@@ -3,9 +3,10 @@
 //
 // Bound: reading A's codes once; a copy of that size reads at 5.4 to 6.3 TB/s in the
 // same 64- and 256-byte runs.  Measured: 65536 x 8192 in 4 bits times an fp32 vector
-// 50 us (5.7 TB/s), A^T of 262144 x 4096 times one 102 (5.6), 131072 x 16384 times 64
-// bf16 columns 325 (3.5: there the matrix cores and X's copies into shared memory
-// take turns with the codes), 11500 x 5750 times 16 14.5 a call, two launches.
+// 50 us (5.7 TB/s), A^T of 262144 x 4096 times one 101 (5.7), times 16 bf16 columns
+// 153 (3.8), 131072 x 16384 times 64 bf16 columns 320 (3.7: there the matrix cores
+// are busy 43% of the cycles and shared memory, X's operands for 32 rows a wave,
+// 27%, and they take turns with the codes), 11500 x 5750 times 16 14.8 a call, two launches.
 //
 // The work for a code is a conversion and the
 // matrix instruction, so neither shared memory nor a second copy holds codes:
@@ -986,6 +987,11 @@ hipError_t launch_mx_join(const MxArgs& a, const float* part, int64_t splits, in
     return hipGetLastError();
 }
 
+// One matrix operand's columns across the blocks, four of them along.  Measured, us, these kernels and the tiles
+// (mx_tiled.hip).  Across, 262144 x 4096: 2 bf16 columns 123 and 253, 16 153 and 266 (17 in tiles 288), 5 fp32 134 and
+// 772 (6: 772); 8 bits, 16 columns 247 and 289; 16384 x 4096, 16: 27.4 and 26.5.  Along, 131072 x 16384: 16 bf16 columns
+// 238 and 545, 64 320 and 592 (65: 742), 21 fp32 328 and 1628; 11500 x 5750: 16 13.5 and 26.4, 32 24.4 and 26.6, 64 44.2
+// and 27.7; 16384 x 4096, 64: 32.5 and 24.1.  So from 33 columns on a matrix of a few thousand rows would be better off in tiles.
 bool mx_few_serves(const MxArgs& a) {
     const int64_t terms = a.trans ? a.q : a.r;
     // offsets within a workgroup's rows, and steps, are 32-bit

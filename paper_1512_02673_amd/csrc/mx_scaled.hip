@@ -8,9 +8,11 @@
 // the same instruction adds with some 14 bits (1e-5 to 5e-5 off, at any length),
 // so those products take the bf16 instructions (mx_tiled.hip) at half its rate.
 //
-// Bound: the matrix cores (16384 x 8192 times 8192
-// columns, bf16 results: 930 us, 2.37 PFLOP/s; the instruction alone, in a loop on
-// registers, 8.5).  The split into tiles, and the way from memory over
+// Bound: waiting.  16384 x 8192 times 8192 columns, bf16 results, takes 870 to 910 us
+// (2.4 to 2.5 PFLOP/s; the instruction alone, in a loop on registers, 8.5): the matrix cores
+// are busy 27% of the cycles, shared memory 26%, and waves wait 42% of their time, at the two
+// barriers of a step and for its loads, since a step's matrix work is a fourth of the
+// bf16 kernel's.  The split into tiles, and the way from memory over
 // registers into shared memory, are those of the products with bf16 (mx_tile.h);
 // no code is converted.  Blocks past the end of a row are zeroed, what lies
 // there need not be numbers; rows past the end are zeros too and not stored.

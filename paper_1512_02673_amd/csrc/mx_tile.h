@@ -41,7 +41,7 @@ inline double step_us(bool large, int64_t groups) {
 // 4.1), or a product with fewer tiles than a round, is cut by the least estimated time: small tiles or large
 // ones, and into how many splits, whose sums are written and read once more.  Measured (large tiles, splits 1 to
 // 16, and small ones): 512 x 4096 of 4096 terms 86 57 41 46 68, 47 41 42 52 70 us; 578 x 6075 of 71240 terms in
-// three planes 4321 2249 1874 1885 1892, 3043 3186 3323 3249 2682; 1000 x 1000 of 16384 terms 307 166 92 63 62,
+// three planes 4321 2249 1874 (1890 with bounded chains) 1885 1892, 3043 3186 3323 3249 2682; 1000 x 1000 of 16384 terms 307 166 92 63 62,
 // 163 95 67 68 72.
 // `chain`: steps of the shorter chain (the workspace is asked for without the results' type).
 inline Cut cut_tiles(int64_t s, int64_t n, int64_t steps, int64_t chain) {

@@ -7,8 +7,9 @@
 // else it goes through the workspace: unpacked from codes, which is exact, or copied,
 // an fp32 X as three planes (split_bf16) whose products are summed one after the
 // other.  There each step's 64 terms of all sides lie together, a side's contiguous
-// and padded with zeros, so that no offset within a step grows with the terms.  Terms
-// past the last one are zeros on one side and finite on the other; rows past the end of A read as zeros.
+// and padded with zeros, so that no offset within a step grows with the terms.
+// Terms past the last one are zeros on one side and finite on the other; rows past
+// the end of A read as zeros.
 //
 // Bound: the matrix cores, and the power they take: they were busy half of the
 // cycles at about 2.1 GHz (operands of zeros instead of data: 10 to 18% faster, a
@@ -17,13 +18,16 @@
 // large one; two such workgroups on a compute unit cover each other's barriers.  A
 // step's operands come from memory into registers while the step before is
 // computed, then into shared memory.  Measured, bf16 results: 16384 x 4096 times
-// 4099 tokens 515 us (1.07 PFLOP/s), its transpose times 4096 tokens 503 (1.09),
-// 16384 x 8192 times 8192 8-bit columns 1920 (1.14), the fp32 gradient 5750 x
-// 11500 of 10000 8-bit tokens 1490 (0.89); a library product of 8192^3 bf16: 1.39 to
-// 1.45.  Tiles of 256 x 128 took 7% longer, 128 x 128 with three workgroups a unit
-// 11 to 15%, 256 x 256 with one 25 to 45%; two halves of shared memory with one
-// barrier a step, wave priorities, and other orders of the reads and matrix
-// instructions were within 2%.
+// 4099 tokens 510 us (1.08 PFLOP/s), its transpose times 4096 tokens 498 (1.10),
+// 16384 x 8192 times 8192 8-bit columns 1930 (1.14), the fp32 gradient 5750 x
+// 11500 of 10000 8-bit tokens 1490 (0.89).  Three planes are three times the work, the
+// codes converted for each: 16384 x 4096 times 4099 fp32 tokens 1540 us (1.07), its
+// transpose times 4096 1660 (0.99), 71240 x 6075 transposed times 578 1890 (0.79; a
+// tenth of its tiles' sides is empty).  A library product
+// of 8192^3 bf16: 1.39 to 1.45.  Tiles of 256 x 128 took 7% longer, 128 x 128 with
+// three workgroups a unit 11 to 15%, 256 x 256 with one 25 to 45%; two halves of shared
+// memory with one barrier a step, wave priorities, and other orders of the reads and
+// matrix instructions were within 2%.
 #include <algorithm>
 
 #include "mx_tile.h"
@@ -36,7 +40,7 @@ constexpr int kStep = 64;   // terms
 struct TileArgs {
     const uint16_t* P;
     int64_t pitch, step, plane; // elements between rows of a step, between steps, and between planes
-    int64_t extent, shrink;     // elements from a step's first to the last that it may read: of the plane's first step, and fewer a step
+    int64_t extent, shrink;     // elements from the first step's first that it may read, and how many fewer each next step may
     int32_t planes;
     int64_t steps;              // of one plane
     Cut cut;
