@@ -168,8 +168,8 @@ def prepare(case, seed):
             if case["bias"]:
                 state["bias"] = torch.randn(q, generator=_generator(seed, 2), device="cuda").to(DT[case["y"]])
         else:
-            state["WT"] = _codes(w.t(), BLOCK)
-            state["XT"] = _codes(_data(s, r, _generator(seed, 1)).t(), 1)
+            state["WT"] = _codes(w.t().contiguous(), BLOCK)
+            state["XT"] = _codes(_data(s, r, _generator(seed, 1)).t().contiguous(), 1)
             state["dY"] = _strided(_data(s, q, _generator(seed, 2), DT[case["x"]], 1 / 256), case["pad"])
             state["dW"] = torch.randn((q, r), generator=_generator(seed, 3), device="cuda")
     elif kind == "dropout":
