@@ -570,6 +570,129 @@ coded_status coded_mx_mm_t(coded_dtype fmt, const void* codes, int64_t ldc, cons
                            double alpha, double beta, const void* C, int64_t ldcc, void* Z, coded_dtype z_dt,
                            int64_t ldz, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------- matrices in 8 bits, blocks of 128
+ * A matrix of q x r as E4M3 codes (values up to 448) with an fp32 scale for each
+ * block of 128 consecutive columns of one row (block_rows 1: activations,
+ * gradients) or of 128 rows (block_rows 128: weights).  Both sides of a product
+ * are such matrices, with the terms of the sum along their rows, so the three
+ * products of a training step read
+ *   forward Y = X W^T:     X (tokens x features) and W (outputs x features),
+ *   dX = dY W:             dY (tokens x outputs) and W^T (features x outputs),
+ *   dW = dY^T X:           dY^T (outputs x tokens) and X^T (features x tokens),
+ * and coded_f8_quantize writes a matrix and its transpose in one pass.
+ *   codes   row t at byte t*ldc (ldc a multiple of 16 that holds a row's whole
+ *           blocks, codes 16-byte aligned), column c in byte c.  The codes that
+ *           fill the last block of a row past column r are zero.
+ *   scales  block b of row t at scales[b*lds + t/block_rows] (lds at least the
+ *           rows' number of blocks; 4-byte aligned).  NaN: a block without
+ *           values, each of them counts as NaN.
+ * Any run of rows that begins at a multiple of block_rows is such a matrix from
+ * its first row and first scale on.  Sizes up to 2^40 each; any may be 0.
+ */
+
+/* The smallest pitches of a q x r matrix: bytes between rows of codes, elements
+ * between rows of scales (one row for each 128 columns).  Either may be NULL. */
+coded_status coded_f8_sizes(int64_t q, int64_t r, int32_t block_rows, int64_t* code_pitch, int64_t* scale_pitch);
+
+/*
+ * coded_f8_quantize -- codes and scales of A (device, q x r of dt = CODED_F32 or
+ * CODED_BF16, row stride lda), of its transpose, or of both in one pass.  With
+ * m the largest magnitude of a block, 2^-100 at least, the scale is m / 448 and
+ * a code is v * (448 / m), each quotient and product rounded to fp32, to the
+ * nearest code, ties to even.  A block with an infinity or NaN in it gets the
+ * scale NaN and codes of zero.
+ *   codes, scales      A's (q x r, blocks of block_rows), or both NULL.
+ *   t_codes, t_scales  its transpose's (r x q, t_block_rows), or both NULL.
+ * Writes whole blocks of codes along a row, nothing behind them.
+ */
+coded_status coded_f8_quantize(coded_dtype dt, const void* A, int64_t q, int64_t r, int64_t lda, int32_t block_rows,
+                               void* codes, int64_t ldc, float* scales, int64_t lds, int32_t t_block_rows,
+                               void* t_codes, int64_t ldtc, float* t_scales, int64_t ldts, void* stream);
+
+/* The values, a code times its scale in fp32, rounded to dt, into out (q x r, row stride ldo). */
+coded_status coded_f8_dequantize(int64_t q, int64_t r, int32_t block_rows, const void* codes, int64_t ldc,
+                                 const float* scales, int64_t lds, coded_dtype dt, void* out, int64_t ldo, void* stream);
+
+/* Bytes of device workspace that coded_f8_mm needs for these sizes (0: none, NULL will do). */
+coded_status coded_f8_workspace(int64_t q, int64_t r, int64_t s, coded_dtype y_dt, int32_t order, int64_t* bytes);
+
+/*
+ * coded_f8_mm -- Y = alpha * A X^T + beta * C, A (q x r) and X (s x r, a
+ * right-hand side a row) in 8 bits.
+ *   order     CODED_Y_ROWS: Y is s x q, a right-hand side a row; else 0: q x s.
+ *   y_dt      CODED_F32: codes' products and their sums are exact products and
+ *             fp32 sums.  CODED_BF16: with more than a few right-hand sides and
+ *             rows, the matrix instruction for 8 bits adds the products of each
+ *             eight consecutive columns to 13 bits below the largest of them
+ *             (at most 7 * 2^-13 of it off, a few 1e-5 of a result in the
+ *             2-norm, where its rounding to bf16 is 1.7e-3); sums of blocks are
+ *             in fp32 in either case, and so is what the scales, alpha and
+ *             beta C add.
+ *   alpha, beta, C, ldcc, Y, ldy, workspace   as coded_mx_mm's.
+ * r up to 2^23 and code pitches up to 2^24 bytes, else CODED_ERR_UNSUPPORTED.  A NaN reaches the
+ * results whose sums it is part of and no other; so does a product of two
+ * blocks' scales that is infinite in fp32.
+ */
+coded_status coded_f8_mm(int64_t q, int64_t r, int64_t s, int32_t block_rows, const void* codes, int64_t ldc,
+                         const float* scales, int64_t lds, int32_t x_block_rows, const void* x_codes, int64_t ldxc,
+                         const float* x_scales, int64_t ldxs, int32_t order, double alpha, double beta, const void* C,
+                         int64_t ldcc, void* Y, coded_dtype y_dt, int64_t ldy, void* workspace, int64_t workspace_bytes,
+                         void* stream);
+
+/* ---------------------------------------------------------------- dropout
+ * coded_dropout -- out = X / (1 - p) where an element is kept, 0 where it is
+ * dropped, plus C (NULL: nothing).  The mask is never stored: it is a function
+ * of seed, draw and the element's place, so the backward pass is the same call
+ * on the gradient, and a worker that holds rows first_row .. first_row + q - 1
+ * of a batch drops what any other does.  With key = output number
+ * (10<<56 | draw) of the counter-based SplitMix64 generator of `seed`, element
+ * (t, c) takes output number (first_row + t) * ceil(r/2) + c/2 of the
+ * generator of `key`, its low 32 bits for even c and its high ones for odd, and
+ * is kept when they are at least p * 2^32 rounded to a whole number.
+ *   dt       CODED_F32 or CODED_BF16, of X, C and out (q x r, row strides ldx,
+ *            ldcc, ldo).  x times 1 / (1 - p), rounded to fp32, plus C is formed
+ *            in fp32 and rounded once.  Dropped infinities and NaN are dropped.
+ *   p        in [0, 1]; 1 drops everything.
+ *   draw     below 2^56.  first_row in [0, 2^40], q and r up to 2^40.
+ * X or C may be out itself, with its stride; they must not overlap it otherwise.
+ */
+coded_status coded_dropout(coded_dtype dt, const void* X, int64_t q, int64_t r, int64_t ldx, double p, uint64_t seed,
+                           uint64_t draw, int64_t first_row, const void* C, int64_t ldcc, void* out, int64_t ldo,
+                           void* stream);
+
+/* ---------------------------------------------------------------- embeddings
+ * Rows of a table by tokens (a product with a matrix whose rows hold a single
+ * one), and the transposed product, the gradient of the table.
+ *   tok       device, n tokens of token_bytes 4 or 8 (int32 or int64).
+ *   skip      a token whose rows are zero and get no gradient (padding); one
+ *             that is no row of the table, -1 for example, skips none.
+ * Table and rows are CODED_F32 or CODED_BF16, each its own; vocab up to 2^31 - 2
+ * rows, n up to 2^31 - 1, d up to 2^40.
+ */
+
+/* out[i] = scale * E[tok[i]] (n x d; scale, the product in fp32, rounded once).
+ * The row of a token that is neither skip nor in [0, vocab) is NaN. */
+coded_status coded_embed(coded_dtype e_dt, const void* E, int64_t vocab, int64_t d, int64_t lde, const void* tok,
+                         int32_t token_bytes, int64_t n, int64_t skip, double scale, coded_dtype out_dt, void* out,
+                         int64_t ldo, void* stream);
+
+/* Bytes of device workspace that coded_embed_grad needs. */
+coded_status coded_embed_workspace(int64_t n, int64_t vocab, int64_t d, int64_t* bytes);
+
+/*
+ * coded_embed_grad -- dE[v] = beta * dE[v] + scale * sum over tok[i] = v of G[i]
+ * (dE vocab x d of e_dt, G n x d of g_dt).  The tokens are sorted and each
+ * row's sum is taken in fp32 in an order that depends on the tokens alone: the
+ * same call gives the same bits.  Tokens that are skip or outside [0, vocab)
+ * add nothing.  With beta == 0 dE is not read and all of it is written; with
+ * beta == 1 the rows of tokens that do not occur are not touched.
+ *   workspace  device, 16-byte aligned, coded_embed_workspace bytes.
+ */
+coded_status coded_embed_grad(coded_dtype g_dt, const void* G, int64_t n, int64_t d, int64_t ldg, const void* tok,
+                              int32_t token_bytes, int64_t vocab, int64_t skip, double scale, double beta,
+                              coded_dtype e_dt, void* dE, int64_t ldde, void* workspace, int64_t workspace_bytes,
+                              void* stream);
+
 #ifdef __cplusplus
 }
 #endif

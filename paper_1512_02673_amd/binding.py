@@ -76,6 +76,20 @@ _SIGNATURES = {
                              _c_i64, _c_i32, _c_dbl, _c_dbl, _c_p, _c_i64, _c_p, _c_i32, _c_i64, _c_p, _c_i64, _c_p]),
     "coded_mx_mm_t": (_c_i32, [_c_i32, _c_p, _c_i64, _c_p, _c_i64, _c_i64, _c_i64, _c_i32, _c_p, _c_i64, _c_i64,
                                _c_i32, _c_dbl, _c_dbl, _c_p, _c_i64, _c_p, _c_i32, _c_i64, _c_p, _c_i64, _c_p]),
+    "coded_f8_sizes": (_c_i32, [_c_i64, _c_i64, _c_i32, _c_p, _c_p]),
+    "coded_f8_quantize": (_c_i32, [_c_i32, _c_p, _c_i64, _c_i64, _c_i64, _c_i32, _c_p, _c_i64, _c_p, _c_i64, _c_i32, _c_p,
+                                   _c_i64, _c_p, _c_i64, _c_p]),
+    "coded_f8_dequantize": (_c_i32, [_c_i64, _c_i64, _c_i32, _c_p, _c_i64, _c_p, _c_i64, _c_i32, _c_p, _c_i64, _c_p]),
+    "coded_f8_workspace": (_c_i32, [_c_i64, _c_i64, _c_i64, _c_i32, _c_i32, _c_p]),
+    "coded_f8_mm": (_c_i32, [_c_i64, _c_i64, _c_i64, _c_i32, _c_p, _c_i64, _c_p, _c_i64, _c_i32, _c_p, _c_i64, _c_p, _c_i64,
+                             _c_i32, _c_dbl, _c_dbl, _c_p, _c_i64, _c_p, _c_i32, _c_i64, _c_p, _c_i64, _c_p]),
+    "coded_dropout": (_c_i32, [_c_i32, _c_p, _c_i64, _c_i64, _c_i64, _c_dbl, _c_u64, _c_u64, _c_i64, _c_p, _c_i64, _c_p, _c_i64,
+                               _c_p]),
+    "coded_embed": (_c_i32, [_c_i32, _c_p, _c_i64, _c_i64, _c_i64, _c_p, _c_i32, _c_i64, _c_i64, _c_dbl, _c_i32, _c_p, _c_i64,
+                             _c_p]),
+    "coded_embed_workspace": (_c_i32, [_c_i64, _c_i64, _c_i64, _c_p]),
+    "coded_embed_grad": (_c_i32, [_c_i32, _c_p, _c_i64, _c_i64, _c_i64, _c_p, _c_i32, _c_i64, _c_i64, _c_dbl, _c_dbl, _c_i32,
+                                  _c_p, _c_i64, _c_p, _c_i64, _c_p]),
     "coded_status_string": (ctypes.c_char_p, [_c_i32]),
     "coded_last_error": (ctypes.c_char_p, []),
     "coded_version": (ctypes.c_char_p, []),
@@ -594,7 +608,7 @@ def _mx_dense(t, name):
         ld, step = t.stride()
     else:
         raise ValueError(f"{name} must be 1-D or 2-D")
-    if cols > 1 and step != 1:
+    if cols > 1 and step != 1 and rows > 0:
         raise ValueError(f"{name} must be row-major")
     return rows, cols, ld if rows > 1 else max(cols, 1), dt
 
@@ -716,3 +730,212 @@ def coded_mx_mm_t(M: MXMatrix, U, Z, x_rows: bool = False, y_rows: bool = False,
     if isinstance(U, MXMatrix):
         raise ValueError("U must be float32 or bfloat16")
     _mx_product(True, M, U, Z, x_rows, y_rows, alpha, beta, C, workspace, stream)
+
+
+# ---------------------------------------------------------------- matrices in 8 bits, dropout, embeddings
+
+def _on_gpu(*named):
+    """Every tensor must be in the current device's memory: another device's, or the host's, would fault there."""
+    for name, t in named:
+        if t is not None and not t.is_cuda:
+            raise ValueError(f"{name} must be on the GPU")
+    device = _torch().cuda.current_device()
+    for name, t in named:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{name} must be on the current device, {device}")
+
+
+def _workspace(nbytes, device, stream):
+    torch = _torch()
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with _memory_of(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+class F8Matrix:
+    """A rows x cols matrix in 8 bits: codes (uint8, rows x code pitch) and scales (float32, a row for every 128
+    columns, an element for every block_rows rows) in the layout of include/coded.h.  block_rows: 1 or 128."""
+
+    __slots__ = ("codes", "scales", "rows_", "cols", "block_rows", "ldc", "lds")
+
+    def __init__(self, codes, scales, rows: int, cols: int, block_rows: int = 1):
+        torch = _torch()
+        if block_rows not in (1, 128):
+            raise ValueError("a block must have 1 or 128 rows")
+        width, blocks, groups = (cols + 127) // 128 * 128, (cols + 127) // 128, (rows + block_rows - 1) // block_rows
+        if codes.dtype is not torch.uint8 or scales.dtype is not torch.float32 or codes.dim() != 2 or scales.dim() != 2:
+            raise ValueError("codes must be uint8 and scales float32, both 2-D")
+        if rows < 0 or cols < 0 or codes.shape[0] != rows or codes.shape[1] < width or (width and codes.stride(1) != 1):
+            raise ValueError(f"codes must be {rows} rows of at least {width} bytes")
+        if scales.shape[0] < blocks or scales.shape[1] < groups or (groups > 1 and scales.stride(1) != 1):
+            raise ValueError(f"scales must be {blocks} rows of at least {groups} elements")
+        self.codes, self.scales, self.rows_, self.cols, self.block_rows = codes, scales, rows, cols, block_rows
+        self.ldc = codes.stride(0) if rows > 1 and cols > 0 else width
+        self.lds = scales.stride(0) if blocks > 1 else groups
+
+    @property
+    def shape(self):
+        return self.rows_, self.cols
+
+    def rows(self, begin: int, end: int) -> "F8Matrix":
+        """Rows begin .. end - 1; begin must be a multiple of block_rows."""
+        if not 0 <= begin <= end <= self.rows_ or begin % self.block_rows:
+            raise ValueError("a run of rows must lie within the matrix and begin with a block")
+        at = begin // self.block_rows
+        return F8Matrix(self.codes[begin:end], self.scales[:, at:], end - begin, self.cols, self.block_rows)
+
+    def _args(self):
+        return self.block_rows, self.codes.data_ptr(), self.ldc, self.scales.data_ptr(), self.lds
+
+
+def coded_f8_sizes(q: int, r: int, block_rows: int = 1):
+    """(code pitch in bytes, scale pitch in elements) of a q x r matrix."""
+    c, s = ctypes.c_int64(), ctypes.c_int64()
+    _check(lib().coded_f8_sizes(q, r, block_rows, ctypes.addressof(c), ctypes.addressof(s)))
+    return c.value, s.value
+
+
+def alloc_f8(q: int, r: int, block_rows: int = 1, device="cuda") -> F8Matrix:
+    """Room for a q x r matrix in 8 bits (not cleared: coded_f8_quantize writes all that is read)."""
+    torch = _torch()
+    if q < 0 or r < 0 or block_rows not in (1, 128):
+        raise ValueError("sizes must be >= 0 and a block have 1 or 128 rows")
+    blocks = (r + 127) // 128
+    return F8Matrix(torch.empty((q, blocks * 128), dtype=torch.uint8, device=device),
+                    torch.empty((blocks, (q + block_rows - 1) // block_rows), dtype=torch.float32, device=device), q, r, block_rows)
+
+
+def coded_f8_quantize(A, M: "F8Matrix | None" = None, MT: "F8Matrix | None" = None, stream=None) -> None:
+    """Codes and scales of A (float32 or bfloat16) into M, of its transpose into MT, or both in one pass."""
+    q, r, lda, dt = _mx_dense(A, "A")
+    if M is None and MT is None:
+        raise ValueError("M or MT must be given")
+    if M is not None and M.shape != (q, r):
+        raise ValueError("M must have A's shape")
+    if MT is not None and MT.shape != (r, q):
+        raise ValueError("MT must have the shape of A's transpose")
+    _on_gpu(("A", A), *((n, t) for n, m in (("M", M), ("MT", MT)) if m is not None for t in (m.codes, m.scales)))
+    none = 1, None, 0, None, 0
+    _check(lib().coded_f8_quantize(dt, A.data_ptr(), q, r, lda, *(none if M is None else M._args()),
+                                   *(none if MT is None else MT._args()), _stream(stream)))
+
+
+def coded_f8_dequantize(M: F8Matrix, out, stream=None) -> None:
+    """M's values into out (float32 or bfloat16)."""
+    q, r, ldo, dt = _mx_dense(out, "out")
+    if M.shape != (q, r):
+        raise ValueError("out must have M's shape")
+    _on_gpu(("out", out), ("M", M.codes), ("M", M.scales))
+    _check(lib().coded_f8_dequantize(q, r, *M._args(), dt, out.data_ptr(), ldo, _stream(stream)))
+
+
+@functools.lru_cache(maxsize=256)
+def coded_f8_workspace(q: int, r: int, s: int, y_dt: int, y_rows: bool = False) -> int:
+    """Bytes of workspace of coded_f8_mm."""
+    b = ctypes.c_int64()
+    _check(lib().coded_f8_workspace(q, r, s, y_dt, bool(y_rows) << 1, ctypes.addressof(b)))
+    return b.value
+
+
+def coded_f8_mm(A: F8Matrix, X: F8Matrix, Y, y_rows: bool = False, alpha: float = 1.0, beta: float = 0.0, C=None,
+                workspace="auto", stream=None) -> None:
+    """Y = alpha * A X^T + beta * C.  A: q x r, X: s x r; Y: q x s (or s x q with y_rows); C: like Y, or one row of it
+    for every row.  A 1-D Y is one right-hand side.  workspace: "auto", or a device buffer of coded_f8_workspace bytes."""
+    q, r = A.shape
+    s, rx = X.shape
+    if rx != r:
+        raise ValueError(f"X must have {r} columns")
+    ny, sy, ldy, y_dt = _mx_side(Y, "Y", y_rows)
+    if ny != q or sy != s:
+        raise ValueError(f"Y must have {q} results for each of {s} right-hand sides")
+    cp, ldcc = None, 0
+    if beta != 0:
+        if C is None or C.dtype != Y.dtype:
+            raise ValueError("C must be given, of Y's type, when beta is not 0")
+        if C.shape == Y.shape:
+            ldcc = _mx_side(C, "C", y_rows)[2]
+        elif C.dim() == 1 and Y.dim() == 2 and C.shape[0] == Y.shape[1] and (C.shape[0] < 2 or C.stride(0) == 1):
+            ldcc = 0   # one row for every row of Y
+        else:
+            raise ValueError("C must have Y's shape, or be one row of it")
+        cp = C.data_ptr()
+    _on_gpu(("Y", Y), ("A", A.codes), ("A", A.scales), ("X", X.codes), ("X", X.scales), ("C", C if beta != 0 else None),
+            ("workspace", None if isinstance(workspace, str) else workspace))
+    wsp, wsb = None, 0
+    if isinstance(workspace, str):
+        wsb = coded_f8_workspace(q, r, s, y_dt, y_rows)
+        if wsb:
+            workspace = _workspace(wsb, Y.device, stream)
+            wsp = workspace.data_ptr()
+    elif workspace is not None:
+        wsp, wsb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(lib().coded_f8_mm(q, r, s, *A._args(), *X._args(), bool(y_rows) << 1, alpha, beta, cp, ldcc, Y.data_ptr(), y_dt, ldy,
+                             wsp, wsb, _stream(stream)))
+
+
+def coded_dropout(X, out, p: float, seed: int, draw: int, first_row: int = 0, C=None, stream=None) -> None:
+    """out = X / (1 - p) where an element is kept and 0 where it is dropped, plus C.  The mask is a function of seed,
+    draw and an element's place; X holds rows first_row .. of the whole batch.  out may be X or C."""
+    q, r, ldx, dt = _mx_dense(X, "X")
+    qo, ro, ldo, dto = _mx_dense(out, "out")
+    if (qo, ro) != (q, r) or dto != dt:
+        raise ValueError("out must have X's shape and type")
+    ldcc = 0
+    if C is not None:
+        qc, rc, ldcc, dtc = _mx_dense(C, "C")
+        if (qc, rc) != (q, r) or dtc != dt:
+            raise ValueError("C must have X's shape and type")
+    if not 0 <= seed < 1 << 64 or not 0 <= draw < 1 << 56:
+        raise ValueError("seed must be in [0, 2^64) and draw in [0, 2^56)")
+    _on_gpu(("X", X), ("out", out), ("C", C))
+    _check(lib().coded_dropout(dt, X.data_ptr(), q, r, ldx, p, seed, draw, first_row, _ptr(C), ldcc, out.data_ptr(), ldo,
+                               _stream(stream)))
+
+
+def _tokens(tok):
+    """(data, bytes a token, tokens) of a contiguous int32 or int64 tensor of any shape."""
+    torch = _torch()
+    if tok.dtype not in (torch.int32, torch.int64) or not tok.is_contiguous():
+        raise ValueError("tokens must be int32 or int64, contiguous")
+    return tok.data_ptr(), tok.element_size(), tok.numel()
+
+
+def coded_embed(E, tok, out, scale: float = 1.0, skip: int = -1, stream=None) -> None:
+    """out[i] = scale * E[tok[i]] (E: vocab x d, out: n x d); zero for the token `skip`, NaN for one that E lacks."""
+    vocab, d, lde, e_dt = _mx_dense(E, "E")
+    n_out, d_out, ldo, out_dt = _mx_dense(out, "out")
+    tp, size, n = _tokens(tok)
+    if E.dim() != 2 or out.dim() != 2 or (n_out, d_out) != (n, d):
+        raise ValueError(f"out must be {n} rows of {d}")
+    _on_gpu(("E", E), ("tok", tok), ("out", out))
+    _check(lib().coded_embed(e_dt, E.data_ptr(), vocab, d, lde, tp, size, n, skip, scale, out_dt, out.data_ptr(), ldo, _stream(stream)))
+
+
+@functools.lru_cache(maxsize=256)
+def coded_embed_workspace(n: int, vocab: int, d: int) -> int:
+    """Bytes of workspace of coded_embed_grad."""
+    b = ctypes.c_int64()
+    _check(lib().coded_embed_workspace(n, vocab, d, ctypes.addressof(b)))
+    return b.value
+
+
+def coded_embed_grad(G, tok, dE, scale: float = 1.0, beta: float = 0.0, skip: int = -1, workspace="auto", stream=None) -> None:
+    """dE[v] = beta * dE[v] + scale * the sum of the rows G[i] with tok[i] == v (G: n x d, dE: vocab x d).
+    workspace: "auto", or a device buffer of coded_embed_workspace bytes."""
+    n_g, d_g, ldg, g_dt = _mx_dense(G, "G")
+    vocab, d, ldde, e_dt = _mx_dense(dE, "dE")
+    tp, size, n = _tokens(tok)
+    if G.dim() != 2 or dE.dim() != 2 or (n_g, d_g) != (n, d):
+        raise ValueError(f"G must be {n} rows of {d}")
+    _on_gpu(("G", G), ("tok", tok), ("dE", dE), ("workspace", None if isinstance(workspace, str) else workspace))
+    wsp, wsb = None, 0
+    if isinstance(workspace, str):
+        wsb = coded_embed_workspace(n, vocab, d)
+        if wsb:
+            workspace = _workspace(wsb, dE.device, stream)
+            wsp = workspace.data_ptr()
+    elif workspace is not None:
+        wsp, wsb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(lib().coded_embed_grad(g_dt, G.data_ptr(), n, d, ldg, tp, size, vocab, skip, scale, beta, e_dt, dE.data_ptr(), ldde, wsp,
+                                  wsb, _stream(stream)))
