@@ -20,7 +20,7 @@ ARCH = "gfx950"
 
 SOURCES = ["api.cpp", "mx_api.cpp", "survivors.cpp", "shuffle.cpp", "encode.hip", "worker.hip", "worker_f32_mfma.hip", "worker_bf16.hip", "fused_bf16.hip",
            "decode.hip", "onepass.hip", "transpose.hip", "runtime.hip", "shuffle.hip", "scratch.hip", "mx_quant.hip",
-           "mx_product.hip", "mx_few.hip", "mx_tiled.hip", "mx_scaled.hip", "f8_api.cpp", "f8_quant.hip", "f8_few.hip",
+           "mx_product.hip", "mx_few.hip", "mx_tiled.hip", "mx_scaled.hip", "f8_api.cpp", "f8_quant.hip", "f8_few.hip", "f8_tiled.hip",
            "layers_api.cpp", "dropout.hip", "embed.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result", f"-I{os.path.join(ROOT, 'include')}"]
@@ -41,7 +41,8 @@ def hipcc() -> str:
 # not overlap with the fp64 matrix work; the fp32 products at s = 16..64
 # measured 5% faster, the others unchanged).
 MFMA_VGPR_FORM = {"worker_f32_mfma.hip", "decode.hip", "worker_bf16.hip", "mx_few.hip",
-                  "mx_tiled.hip", "mx_scaled.hip", "f8_few.hip"}
+                  "mx_tiled.hip", "mx_scaled.hip", "f8_few.hip",
+                  "f8_tiled.hip"}
 
 
 def _compile(src: str, verbose: bool) -> str:

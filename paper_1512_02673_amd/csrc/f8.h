@@ -40,6 +40,10 @@ bool f8_few_serves(const F8Args& a);
 int64_t f8_few_workspace_bytes(const F8Args& a);
 hipError_t launch_f8_few(const F8Args& a, hipStream_t st);
 
+// Many of both (f8_tiled.hip); results of a right-hand side in a row of Y.
+int64_t f8_tiled_workspace_bytes(const F8Args& a);
+hipError_t launch_f8_tiled(const F8Args& a, hipStream_t st);
+
 #ifdef __HIPCC__
 // Eight codes (two words) as a bf16 operand of the matrix instructions, exact.
 __device__ __forceinline__ bf16x8 f8_to_bf16(uint32_t lo, uint32_t hi) {

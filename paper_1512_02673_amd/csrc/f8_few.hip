@@ -9,6 +9,7 @@
 // Where there are few workgroups the blocks are split among several, whose sums
 // are joined in order.
 #include <algorithm>
+#include <utility>
 
 #include "f8.h"
 
@@ -121,7 +122,7 @@ Plan plan_of(const F8Args& a) {
 
 }  // namespace
 
-bool f8_few_serves(const F8Args&) { return true; }
+bool f8_few_serves(const F8Args& a) { return a.o.s <= 64; }
 
 int64_t f8_few_workspace_bytes(const F8Args& a) {
     const Plan p = plan_of(a);
@@ -141,8 +142,26 @@ hipError_t launch_f8_few(const F8Args& a, hipStream_t st) {
     return p.splits > 1 ? launch_mx_join(a.o, g.part, p.splits, a.o.q, st) : hipSuccess;
 }
 
-int64_t f8_workspace_bytes(const F8Args& a) { return f8_few_workspace_bytes(a); }
+// The sides change places where Y has the other order: the tiles write rows of it, and few results of many
+// right-hand sides are few right-hand sides with many results.
+static F8Args arranged(F8Args a) {
+    const bool turn = f8_few_serves(a) ? false : a.o.q <= 64 ? true : !a.o.y_rows;
+    if (turn) {
+        std::swap(a.P, a.Q);
+        std::swap(a.o.q, a.o.s);
+        a.o.y_rows = !a.o.y_rows;
+    }
+    return a;
+}
 
-hipError_t launch_f8_product(F8Args a, hipStream_t st) { return launch_f8_few(a, st); }
+int64_t f8_workspace_bytes(const F8Args& given) {
+    const F8Args a = arranged(given);
+    return f8_few_serves(a) ? f8_few_workspace_bytes(a) : f8_tiled_workspace_bytes(a);
+}
+
+hipError_t launch_f8_product(F8Args given, hipStream_t st) {
+    const F8Args a = arranged(given);
+    return f8_few_serves(a) ? launch_f8_few(a, st) : launch_f8_tiled(a, st);
+}
 
 }  // namespace coded
