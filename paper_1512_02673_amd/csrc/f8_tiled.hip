@@ -23,6 +23,7 @@ namespace coded {
 namespace {
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 512;
 constexpr int64_t kMostChain = 4096;   // blocks that one fp32 sum takes: 2^-12 of the magnitudes at the most, next to 128 terms' 2^-16 each
@@ -64,251 +65,278 @@ __device__ __forceinline__ Place tile_place(const Cut& c, int64_t b) {
     return place_of(c, x * base + lesser(x, more) + b / 8);
 }
 
-// A lane's results: right-hand side 16 x + li of its wave's, results (4 lk + e) TJ + y, alpha times the sums plus beta C.
-template <int TI, int TJ, int WI>
-__device__ __forceinline__ void put_results(const MxArgs& o, int64_t i0, int64_t j0, const f32x4_t (&acc)[TI][TJ]) {
-    const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4, wave = threadIdx.x >> 6;
-    const int64_t i1 = i0 + wave % WI * TI * 16, j1 = j0 + wave / WI * TJ * 16 + 4 * lk * TJ;
+// `N` neighbouring results of a right-hand side, alpha times the sums plus beta C.
+template <int N, bool BF16>
+__device__ __forceinline__ void put_some(const MxArgs& o, int64_t i, int64_t j, float (&v)[N]) {
+    typedef float wide_t __attribute__((ext_vector_type(N)));
+    typedef wide_t wide_f __attribute__((aligned(4)));
+    typedef uint16_t half_t __attribute__((ext_vector_type(N)));
+    typedef half_t half_b __attribute__((aligned(2)));
+    wide_t w;
+#pragma unroll
+    for (int y = 0; y < N; ++y) w[y] = v[y] * o.alpha;
+    if (o.C) {
+        wide_t c;
+        if constexpr (BF16) {
+            const half_t h = *reinterpret_cast<const half_b*>(static_cast<const uint16_t*>(o.C) + i * o.ldcc + j);
+#pragma unroll
+            for (int y = 0; y < N; ++y) c[y] = __uint_as_float(static_cast<uint32_t>(h[y]) << 16);
+        } else {
+            c = *reinterpret_cast<const wide_f*>(static_cast<const float*>(o.C) + i * o.ldcc + j);
+        }
+#pragma unroll
+        for (int y = 0; y < N; ++y) w[y] = fmaf(o.beta, c[y], w[y]);
+    }
+    if constexpr (BF16) {
+        half_t h;
+#pragma unroll
+        for (int y = 0; y < N; ++y) h[y] = mx_to_bf16(w[y]);
+        *reinterpret_cast<half_b*>(static_cast<uint16_t*>(o.Y) + i * o.ldy + j) = h;
+    } else {
+        *reinterpret_cast<wide_f*>(static_cast<float*>(o.Y) + i * o.ldy + j) = w;
+    }
+}
+
+// A lane's results: right-hand side 32 x + l31 of its wave's, results (8 a + 4 h + b) TJ + y.
+template <int TI, int TJ, int WI, bool BF16>
+__device__ __forceinline__ void put_results(const MxArgs& o, int64_t i0, int64_t j0, const f32x4_t (&acc)[TI][TJ][4]) {
+    constexpr int N = TJ == 1 ? 4 : 8;   // at a time
+    const int lane = threadIdx.x & 63, l31 = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t i1 = i0 + wave % WI * TI * 32 + l31, j1 = j0 + wave / WI * TJ * 32;
+    const bool whole = j1 + 32 * TJ <= o.q;   // the same for the wave
 #pragma unroll
     for (int x = 0; x < TI; ++x) {
-        const int64_t i = i1 + 16 * x + li;
+        const int64_t i = i1 + 32 * x;
         if (i >= o.s) continue;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int64_t j = j1 + e * TJ;
-            if constexpr (TJ == 8) {
-                float v[8];
+        for (int k = 0; k < 16 * TJ / N; ++k) {
+            const int a = k * N / (4 * TJ), in = k * N % (4 * TJ);
+            const int64_t j = j1 + (8 * a + 4 * h) * TJ + in;
+            float v[N];
 #pragma unroll
-                for (int y = 0; y < 8; ++y) v[y] = acc[x][y][e] * o.alpha;
-                if (j >= o.q) continue;
-                if (o.C) {
-                    float c[8];
-                    if (o.y_bf16)
-                        row_load<true>(static_cast<const uint16_t*>(o.C) + i * o.ldcc, j, o.q, c);
-                    else
-                        row_load<false>(static_cast<const float*>(o.C) + i * o.ldcc, j, o.q, c);
-#pragma unroll
-                    for (int y = 0; y < 8; ++y) v[y] = fmaf(o.beta, c[y], v[y]);
-                }
-                if (o.y_bf16)
-                    row_store<true>(static_cast<uint16_t*>(o.Y) + i * o.ldy, j, o.q, v);
-                else
-                    row_store<false>(static_cast<float*>(o.Y) + i * o.ldy, j, o.q, v);
+            for (int e = 0; e < N; ++e) v[e] = acc[x][(in + e) % TJ][a][(in + e) / TJ];
+            if (whole) {
+                put_some<N, BF16>(o, i, j, v);
             } else {
-                if (TJ == 4 && !o.y_bf16 && j + 4 <= o.q) {
-                    f32x4_t v = {acc[x][0][e], acc[x][1][e], acc[x][2 % TJ][e], acc[x][3 % TJ][e]};
-                    v *= o.alpha;
-                    if (o.C) {
-                        const f32x4_t c = *reinterpret_cast<const f32x4_any*>(static_cast<const float*>(o.C) + i * o.ldcc + j);
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) v[y] = fmaf(o.beta, c[y], v[y]);
-                    }
-                    *reinterpret_cast<f32x4_any*>(static_cast<float*>(o.Y) + i * o.ldy + j) = v;
-                    continue;
+                for (int e = 0; e < N; ++e) {
+                    float u[1] = {v[e]};
+                    if (j + e < o.q) put_some<1, BF16>(o, i, j + e, u);
                 }
-#pragma unroll
-                for (int y = 0; y < TJ; ++y)
-                    if (j + y < o.q) mx_store(o, i, j + y, acc[x][y][e]);
             }
         }
     }
 }
 
-// TI x TJ tiles of 16 x 16 a wave, WI waves along the right-hand sides and 8 / WI along the results.  ACC: by way of
+// 16 or 4 bytes a lane from `from` bytes on, to `to` in shared memory (the wave's first lane's; the others' follow).
+__device__ __forceinline__ void sixteen_to_shared(const Window& w, char* to, uint32_t from) {
+#ifdef __HIP_DEVICE_COMPILE__   // the host's pass knows no such load, and would drop the kernel
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(w.rsrc, (__attribute__((address_space(3))) void*)to, 16, from, 0, 0, 0);
+#endif
+}
+__device__ __forceinline__ void four_to_shared(const Window& w, char* to, uint32_t from) {
+#ifdef __HIP_DEVICE_COMPILE__
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(w.rsrc, (__attribute__((address_space(3))) void*)to, 4, from, 0, 0, 0);
+#endif
+}
+
+// TI x TJ tiles of 32 x 32 a wave, WI waves along the right-hand sides and 8 / WI along the results.  ACC: by way of
 // bf16.  MODE 0: Q's scales are the same for a wave's results (blocks of 128 rows), 1: P's for its right-hand sides,
 // 2: neither is taken to be.
 template <int TI, int TJ, int WI, bool ACC, int MODE>
 __global__ __launch_bounds__(kThreads, 2) void f8_tile_kernel(TileArgs g) {
-    constexpr int WJ = 8 / WI, BI = 16 * TI * WI, BJ = 16 * TJ * WJ, kRows = BI + BJ;
-    constexpr int kPieces = kRows * 8 / kThreads;   // of 16 bytes a thread loads of a step
-    constexpr int kPP = BI * 8 / kThreads;          // of these, P's
-    static_assert(BI * 8 % kThreads == 0 && BJ * 8 % kThreads == 0 && kRows <= kThreads, "rows must split evenly over the threads");
-    static_assert(MODE != 0 || 128 % (16 * TJ) == 0, "a wave's results must lie in a block");
-    static_assert(MODE != 1 || 128 % (16 * TI) == 0, "a wave's right-hand sides must lie in a block");
-    extern __shared__ __attribute__((aligned(16))) char smem[];
-    float* const scales = reinterpret_cast<float*>(smem + 2 * kRows * kF8Block);
-    const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
+    constexpr int WJ = 8 / WI, BI = 32 * TI * WI, BJ = 32 * TJ * WJ, kRows = BI + BJ;
+    constexpr int kLoads = kRows / 64;   // of 1 KB, eight rows, a wave has of a step
+    static_assert(kRows % 64 == 0 && kRows <= kThreads, "rows must split evenly over the waves");
+    static_assert(MODE != 0 || 128 % (32 * TJ) == 0, "a wave's results must lie in a block");
+    static_assert(MODE != 1 || 128 % (32 * TI) == 0, "a wave's right-hand sides must lie in a block");
+    // Two halves, of one step's codes and then scales each: two arrays, so that reads of one do not wait for what is
+    // on its way into the other.
+    __shared__ __attribute__((aligned(16))) char half0[kRows * kF8Block + kThreads * 4];
+    __shared__ __attribute__((aligned(16))) char half1[kRows * kF8Block + kThreads * 4];
+    const int tid = threadIdx.x, lane = tid & 63, l31 = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wi = wave % WI * TI * 16, wj = wave / WI * TJ * 16;
+    const int wi = wave % WI * TI * 32, wj = wave / WI * TJ * 32;
     const MxArgs& o = g.a.o;
     const F8Mat &P = g.a.P, &Q = g.a.Q;
     const Place place = tile_place(g.cut, g.first + blockIdx.x);
     const int64_t i0 = place.i * BI, j0 = place.j * BJ;
 
-    // What this thread loads of a step: pieces tid % 8 of rows tid / 8, 64 more, and so on.  Rows past the last one
-    // read as zeros, and are not stored.
-    const int row = tid >> 3, piece = tid & 7;
-    const uint32_t p_from = static_cast<uint32_t>(row * P.ldc) + piece * 16, q_from = static_cast<uint32_t>(row * Q.ldc) + piece * 16;
-    const auto place_in = [&](int at) { return at * kF8Block + (piece ^ ((at >> 1) & 7)) * 16; };
-    const auto q_row = [](int r) { return r - r % (16 * TJ) + r % (16 * TJ) % TJ * 16 + r % (16 * TJ) / TJ; };
-    const int p_to = place_in(row), q_to = place_in(BI + q_row(row));
-    // 64 rows on: the same place within another wave's results, or eight rows further among 128 (another swizzle)
-    [[maybe_unused]] const int q_to_odd = place_in(BI + q_row(row + 64));
-    const int srow = tid < BI ? tid : lesser(tid, kRows - 1) - BI;
-    const int64_t sfrom = tid < BI ? lesser(i0 + srow, o.s - 1) / P.block_rows : lesser(j0 + srow, o.q - 1) / Q.block_rows;
-    const int sto = tid < BI ? srow : BI + q_row(srow);
+    // Which row of the tile lies at place `at`: Q's in the order that the results come out in.  Rows past the last one
+    // repeat it, and are not stored: all loads lie within the matrices.
+    const auto q_row = [](int at) { return at - at % (32 * TJ) + at % 32 * TJ + at % (32 * TJ) / 32; };
+    uint32_t from[kLoads];
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) {
+        const int at = (wave * kLoads + l) * 8 + (lane >> 3), piece = (lane & 7) ^ ((at >> 1) & 7);
+        from[l] = static_cast<uint32_t>(at < BI ? lesser(at, o.s - 1 - i0) * P.ldc : lesser(q_row(at - BI), o.q - 1 - j0) * Q.ldc) + piece * 16;
+    }
+    const int sat = wave * 64 + lane;   // the place whose scale this lane loads
+    const int p_log = P.block_rows == 1 ? 0 : 7, q_log = Q.block_rows == 1 ? 0 : 7;
+    const uint32_t s_from = 4 * static_cast<uint32_t>(sat < BI ? (lesser(i0 + sat, o.s - 1) >> p_log) - (i0 >> p_log)
+                                                               : (lesser(j0 + q_row(lesser(sat, kRows - 1) - BI), o.q - 1) >> q_log) - (j0 >> q_log));
     const int64_t t0 = place.split < 0 ? 0 : place.split * g.cut.per;
     const int64_t t1 = place.split < 0 ? g.a.blocks : lesser(t0 + g.cut.per, g.a.blocks);
+    // a wave's loads and scales are all of one side
     const uint8_t* p_base = P.codes + i0 * P.ldc + t0 * kF8Block;
     const uint8_t* q_base = Q.codes + j0 * Q.ldc + t0 * kF8Block;
-    int64_t p_left = (o.s - 1 - i0) * P.ldc + (g.a.blocks - t0) * kF8Block, q_left = (o.q - 1 - j0) * Q.ldc + (g.a.blocks - t0) * kF8Block;
-    const float* s_base = tid < BI ? P.scales + t0 * P.lds + sfrom : Q.scales + t0 * Q.lds + sfrom;
-    const int64_t s_step = tid < BI ? P.lds : Q.lds;
-    const uint32_t p_far = static_cast<uint32_t>(64 * P.ldc), q_far = static_cast<uint32_t>(64 * Q.ldc);
-    u32x4_t next[kPieces];
-    float s_next;
-    const auto fetch = [&] {
-        const Window p(p_base, p_left), q(q_base, q_left);
+    const bool s_of_p = wave * 64 < BI;
+    const float* s_base = s_of_p ? P.scales + t0 * P.lds + (i0 >> p_log) : Q.scales + t0 * Q.lds + (j0 >> q_log);
+    const int64_t s_step = s_of_p ? P.lds : Q.lds;
+    int64_t steps = t1 - t0, ahead = steps;   // of them not fetched yet
+    const auto fetch = [&](char* half) {
+        const Window p(p_base, 0xFFFFFFFF), q(q_base, 0xFFFFFFFF), sc(s_base, 0xFFFFFFFF);
 #pragma unroll
-        for (int l = 0; l < kPieces; ++l) next[l] = l < kPP ? p.four(p_from + l * p_far) : q.four(q_from + (l - kPP) * q_far);
-        s_next = *s_base;
+        for (int l = 0; l < kLoads; ++l) {
+            const int at = (wave * kLoads + l) * 8;
+            sixteen_to_shared(at < BI ? p : q, half + at * kF8Block, from[l]);
+        }
+        four_to_shared(sc, half + kRows * kF8Block + wave * 256, s_from);
+        if (--ahead <= 0) return;   // the last step is fetched again: loads under a condition would be waited for at once
         p_base += kF8Block;
         q_base += kF8Block;
-        p_left -= kF8Block;
-        q_left -= kF8Block;
         s_base += s_step;
     };
-    const auto stage = [&](int half) {
-        char* const codes = smem + half * (kRows * kF8Block);
-#pragma unroll
-        for (int l = 0; l < kPieces; ++l) {
-            const int k = l - kPP;
-            const int to = l < kPP ? p_to + l * 64 * kF8Block
-                           : TJ == 8 ? (k & 1 ? q_to_odd : q_to) + k / 2 * 128 * kF8Block
-                                     : q_to + k * 64 * kF8Block;
-            *reinterpret_cast<u32x4_t*>(codes + to) = next[l];
-        }
-        if (tid < kRows) scales[half * kRows + sto] = s_next;
-    };
 
-    f32x4_t acc[TI][TJ] = {};
-    // where this lane's two pieces of a row lie: rows of a tile differ in the swizzle by li alone
-    const int at0 = (lk ^ ((li >> 1) & 7)) * 16 + li * kF8Block, at1 = at0 ^ 64;
-    const auto compute = [&](int half) {
-        const char* const codes = smem + half * (kRows * kF8Block);
-        const float* const sp = scales + half * kRows + wi;
-        const float* const sq = scales + half * kRows + BI + wj;
-        const auto raw = [&](int row, u32x4_t (&w)[2]) {
-            w[0] = *reinterpret_cast<const u32x4_t*>(codes + row * kF8Block + at0);
-            w[1] = *reinterpret_cast<const u32x4_t*>(codes + row * kF8Block + at1);
-        };
+    f32x4_t acc[TI][TJ][4] = {};
+    // One step.  Pieces of a row lie exchanged by the row's place, (at >> 1) & 7: the 16-byte reads of sixteen lanes
+    // together, eight pairs of rows, fill all banks.  This lane's pieces of a row are 2 h and 2 h + 1 of either half.
+    const auto multiply = [&](const char* half) {
+        const float* const sp = reinterpret_cast<const float*>(half + kRows * kF8Block) + wi;
+        const float* const sq = reinterpret_cast<const float*>(half + kRows * kF8Block) + BI + wj;
+        int own = l31 * kF8Block + (((2 * h) ^ (l31 >> 1)) & 7) * 16;
+        asm volatile("" : "+v"(own));   // addresses are formed anew each step: kept, they would take registers from the sums
+        const auto piece = [&](int row, int c) { return *reinterpret_cast<const u32x4_t*>(half + row * kF8Block + (own ^ (c / 2 * 64 + c % 2 * 16))); };
         float f[TI];
-        [[maybe_unused]] const float one = MODE == 0 ? sq[0] : sp[0];
+        [[maybe_unused]] float one = 1.0f;
+        f32x4_t by[4];
+        const auto scales_of = [&](int y) {
+            if constexpr (MODE != 0)
 #pragma unroll
-        for (int x = 0; x < TI; ++x) f[x] = MODE == 1 ? 1.0f : sp[16 * x + li];
+                for (int a = 0; a < 4; ++a) {
+                    by[a] = *reinterpret_cast<const f32x4_t*>(sq + 32 * y + 8 * a + 4 * h);
+                    if constexpr (MODE == 1) by[a] *= one;
+                }
+        };
+        const auto add = [&](int x, int y, const f32x16_t& v) {
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float w = v[4 * a + e];
+                    acc[x][y][a][e] = MODE == 0   ? fmaf(w, f[x], acc[x][y][a][e])
+                                      : MODE == 1 ? fmaf(w, by[a][e], acc[x][y][a][e])
+                                                  : fmaf(w * f[x], by[a][e], acc[x][y][a][e]);
+                }
+                asm volatile("" : "+v"(acc[x][y][a]));   // here, and not behind all the matrix instructions
+            }
+        };
+        u32x4_t qw[2][2], pw[TI][4];
+        qw[0][0] = piece(BI + wj, 0);
+        qw[0][1] = piece(BI + wj, 1);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int x = 0; x < TI; ++x) pw[x][c] = piece(wi + 32 * x, c);
+        if constexpr (MODE != 2) one = MODE == 0 ? sq[0] : sp[0];
+#pragma unroll
+        for (int x = 0; x < TI; ++x) f[x] = MODE == 1 ? 1.0f : sp[32 * x + l31];
         if constexpr (MODE == 0) {
 #pragma unroll
             for (int x = 0; x < TI; ++x) f[x] *= one;
         }
-        const auto add = [&](int x, int y, f32x4_t t, f32x4_t by) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                acc[x][y][e] = MODE == 0   ? fmaf(t[e], f[x], acc[x][y][e])
-                               : MODE == 1 ? fmaf(t[e], by[e], acc[x][y][e])
-                                           : fmaf(t[e] * f[x], by[e], acc[x][y][e]);
-        };
-        const auto scales_of = [&](int y) {
-            f32x4_t by = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (MODE != 0) by = *reinterpret_cast<const f32x4_t*>(sq + 16 * y + 4 * lk);
-            if constexpr (MODE == 1) by *= one;
-            return by;
-        };
-        u32x4_t pw[TI][2];
-#pragma unroll
-        for (int x = 0; x < TI; ++x) raw(wi + 16 * x, pw[x]);
-        if constexpr (ACC) {
-            bf16x8 pv[TI][4];
+        [[maybe_unused]] bf16x8 pv[TI][8];
+        if constexpr (ACC)
 #pragma unroll
             for (int x = 0; x < TI; ++x)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) pv[x][u] = f8_to_bf16(pw[x][u / 2][u % 2 * 2], pw[x][u / 2][u % 2 * 2 + 1]);
+                for (int u = 0; u < 8; ++u) pv[x][u] = f8_to_bf16(pw[x][u / 2][u % 2 * 2], pw[x][u / 2][u % 2 * 2 + 1]);
+        const f32x16_t zero = {};
+        f32x16_t t[TI];
 #pragma unroll
-            for (int y = 0; y < TJ; ++y) {
-                u32x4_t qw[2];
-                raw(BI + wj + 16 * y, qw);
-                const f32x4_t by = scales_of(y);
-                bf16x8 qv[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) qv[u] = f8_to_bf16(qw[u / 2][u % 2 * 2], qw[u / 2][u % 2 * 2 + 1]);
-                f32x4_t t[TI] = {};
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-#pragma unroll
-                    for (int x = 0; x < TI; ++x) t[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qv[u], pv[x][u], t[x], 0, 0, 0);
-#pragma unroll
-                for (int x = 0; x < TI; ++x) add(x, y, t[x], by);
+        for (int m = 0; m < 2 * TJ; ++m) {   // tile row m / 2, half m % 2 of the block
+            const int y = m / 2, u = m % 2;
+            if (m + 1 < 2 * TJ) {
+                qw[(m + 1) & 1][0] = piece(BI + wj + 32 * ((m + 1) / 2), (m + 1) % 2 * 2);
+                qw[(m + 1) & 1][1] = piece(BI + wj + 32 * ((m + 1) / 2), (m + 1) % 2 * 2 + 1);
             }
-        } else {
-            // Q's operand and scales one tile row ahead, what an instruction gave two instructions behind
-            u32x4_t qw[2][2];
-            f32x4_t by[3], t[3];
-            raw(BI + wj, qw[0]);
-            by[0] = scales_of(0);
+            if constexpr (ACC) {
 #pragma unroll
-            for (int y = 0; y < TJ; ++y) {
-                if (y + 1 < TJ) {
-                    raw(BI + wj + 16 * (y + 1), qw[(y + 1) & 1]);
-                    by[(y + 1) % 3] = scales_of(y + 1);
+                for (int k = 0; k < 4; ++k) {
+                    const bf16x8 qv = f8_to_bf16(qw[u][k / 2][k % 2 * 2], qw[u][k / 2][k % 2 * 2 + 1]);
+#pragma unroll
+                    for (int x = 0; x < TI; ++x) {
+                        if (m > 0 && u == 0 && k == 0) add(x, y - 1, t[x]);
+                        t[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qv, pv[x][4 * u + k], u + k ? t[x] : zero, 0, 0, 0);
+                        asm volatile("" : "+v"(t[x]));
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
-                const i32x8_t qv = __builtin_bit_cast(i32x8_t, __builtin_shufflevector(qw[y & 1][0], qw[y & 1][1], 0, 1, 2, 3, 4, 5, 6, 7));
+            } else {
+                const i32x8_t qo = __builtin_bit_cast(i32x8_t, __builtin_shufflevector(qw[u][0], qw[u][1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
                 for (int x = 0; x < TI; ++x) {
-                    const int n = y * TI + x;
-                    const i32x8_t px = __builtin_bit_cast(i32x8_t, __builtin_shufflevector(pw[x][0], pw[x][1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    t[n % 3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(qv, px, f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-                    asm volatile("" : "+v"(t[n % 3]));
-                    if (n >= 2) {
-                        const int px_ = (n - 2) % TI, py = (n - 2) / TI;
-                        add(px_, py, t[(n - 2) % 3], by[py % 3]);
-                        asm volatile("" : "+v"(acc[px_][py]));   // here, and not behind all the matrix instructions
-                    }
+                    const i32x8_t po = __builtin_bit_cast(i32x8_t, __builtin_shufflevector(pw[x][2 * u], pw[x][2 * u + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    if (m > 0 && u == 0) add(x, y - 1, t[x]);
+                    t[x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(qo, po, u ? t[x] : zero, 0, 0, 0, 0, 0, 0);
+                    asm volatile("" : "+v"(t[x]));
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-#pragma unroll
-            for (int n = TI * TJ - 2; n < TI * TJ; ++n) add(n % TI, n / TI, t[n % 3], by[n / TI % 3]);
+            if (u == 0) scales_of(y);
         }
+#pragma unroll
+        for (int x = 0; x < TI; ++x) add(x, TJ - 1, t[x]);
+    };
+    // What this wave loaded into shared memory is there, and every wave is here and has read what it wanted.
+    const auto meet = [] {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
     };
 
-    if (t0 < t1) {
-        fetch();
-        stage(0);
+    if (steps & 1) {   // an odd number: one by itself, so that the loop has one way out
+        fetch(half1);
+        meet();
+        fetch(half0);
+        multiply(half1);
+    } else if (steps) {
+        fetch(half0);
     }
-    for (int64_t t = t0; t < t1; ++t) {
-        const int half = static_cast<int>(t - t0) & 1;
-        __syncthreads();
-        if (t + 1 < t1) fetch();
-        compute(half);
-        if (t + 1 < t1) stage(half ^ 1);
+    for (steps &= ~int64_t(1); steps > 0; steps -= 2) {
+        meet();
+        fetch(half1);
+        multiply(half0);
+        meet();
+        fetch(half0);
+        multiply(half1);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // shared memory is another workgroup's after this one
     if (place.split < 0) {
-        put_results<TI, TJ, WI>(o, i0, j0, acc);
+        put_results<TI, TJ, WI, !ACC>(o, i0, j0, acc);
     } else {
         float* const part = g.part + (place.split * g.cut.rest() + place.shared) * (BI * BJ);
 #pragma unroll
-        for (int x = 0; x < TI; ++x)
-#pragma unroll
-            for (int y = 0; y < TJ; ++y) *reinterpret_cast<f32x4_t*>(part + ((x * TJ + y) * kThreads + tid) * 4) = acc[x][y];
+        for (int n = 0; n < 4 * TI * TJ; ++n) *reinterpret_cast<f32x4_t*>(part + (n * kThreads + tid) * 4) = acc[n / (4 * TJ)][n / 4 % TJ][n % 4];
     }
 }
 
 // The shared tiles' results from the sums of their splits, added in order.
-template <int TI, int TJ, int WI>
+template <int TI, int TJ, int WI, bool BF16>
 __global__ __launch_bounds__(kThreads) void f8_shared_kernel(TileArgs g) {
-    constexpr int BI = 16 * TI * WI, BJ = 16 * TJ * (8 / WI);
+    constexpr int BI = 32 * TI * WI, BJ = 32 * TJ * (8 / WI);
     const Place p = place_of(g.cut, g.cut.whole + blockIdx.x);
-    f32x4_t acc[TI][TJ] = {};
+    f32x4_t acc[TI][TJ][4] = {};
     for (int64_t k = 0; k < g.cut.splits; ++k) {
         const float* const part = g.part + (k * g.cut.rest() + blockIdx.x) * (BI * BJ);
 #pragma unroll
-        for (int x = 0; x < TI; ++x)
-#pragma unroll
-            for (int y = 0; y < TJ; ++y) acc[x][y] += *reinterpret_cast<const f32x4_t*>(part + ((x * TJ + y) * kThreads + threadIdx.x) * 4);
+        for (int n = 0; n < 4 * TI * TJ; ++n) acc[n / (4 * TJ)][n / 4 % TJ][n % 4] += *reinterpret_cast<const f32x4_t*>(part + (n * kThreads + threadIdx.x) * 4);
     }
-    put_results<TI, TJ, WI>(g.a.o, p.i * BI, p.j * BJ, acc);
+    put_results<TI, TJ, WI, BF16>(g.a.o, p.i * BI, p.j * BJ, acc);
 }
-
-constexpr int64_t lds_bytes(int64_t rows) { return 2 * rows * (kF8Block + 4); }
 
 // Large tiles: 256 x 256 on the 8-bit instruction, 128 x 256 by way of bf16; else 64 x 128.
 Cut cut_of(const F8Args& a) {
@@ -321,7 +349,7 @@ Cut cut_of(const F8Args& a) {
         c.bj = large ? 256 : 128;
         c.tiles_i = ceil_div(a.o.s, c.bi);
         c.tiles_j = ceil_div(a.o.q, c.bj);
-        const double step = large ? 2.2 : 0.5;   // us of a block
+        const double step = large ? 2.0 : 1.0;   // us of a block
         const int64_t round = large ? 256 : 512, tiles = c.tiles_i * c.tiles_j, whole = tiles / round * round;
         for (int64_t splits = 1; splits <= 64; splits *= 2) {
             if (splits > 1 && (splits > a.blocks / 2 || (tiles - whole) * splits > 2 * round)) break;
@@ -346,17 +374,16 @@ Cut cut_of(const F8Args& a) {
 
 template <int TI, int TJ, int WI, bool ACC, int MODE>
 hipError_t launch_tiles(TileArgs g, hipStream_t st) {
-    constexpr int64_t kRows = 16 * TI * WI + 16 * TJ * (8 / WI), kLds = lds_bytes(kRows);
     const auto kernel = f8_tile_kernel<TI, TJ, WI, ACC, MODE>;
     const int64_t all = g.cut.groups(), most = int64_t(1) << 22;
     for (; g.first < all; g.first += most) {
-        kernel<<<dim3(static_cast<uint32_t>(lesser(most, all - g.first))), kThreads, kLds, st>>>(g);
+        kernel<<<dim3(static_cast<uint32_t>(lesser(most, all - g.first))), kThreads, 0, st>>>(g);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (g.cut.splits <= 1) return hipSuccess;
     if (!grid_fits(g.cut.rest(), kThreads)) return hipErrorInvalidConfiguration;
-    f8_shared_kernel<TI, TJ, WI><<<dim3(static_cast<uint32_t>(g.cut.rest())), kThreads, 0, st>>>(g);
+    f8_shared_kernel<TI, TJ, WI, !ACC><<<dim3(static_cast<uint32_t>(g.cut.rest())), kThreads, 0, st>>>(g);
     return hipGetLastError();
 }
 
@@ -374,8 +401,8 @@ int64_t f8_tiled_workspace_bytes(const F8Args& a) { return cut_of(a).part_bytes(
 hipError_t launch_f8_tiled(const F8Args& a, hipStream_t st) {
     TileArgs g{a, cut_of(a), 0, static_cast<float*>(a.o.workspace)};
     const bool acc = !a.o.y_bf16, large = g.cut.bj == 256;
-    if (!large) return acc ? launch_tiles<2, 2, 2, true, 2>(g, st) : launch_tiles<2, 2, 2, false, 2>(g, st);
-    return acc ? launch_large<4, 4, 2, true>(g, st) : launch_large<4, 8, 4, false>(g, st);
+    if (!large) return acc ? launch_tiles<1, 1, 2, true, 2>(g, st) : launch_tiles<1, 1, 2, false, 2>(g, st);
+    return acc ? launch_large<2, 2, 2, true>(g, st) : launch_large<2, 4, 4, false>(g, st);
 }
 
 }  // namespace coded
