@@ -67,7 +67,7 @@ __device__ __forceinline__ Place tile_place(const Cut& c, int64_t b) {
 
 // `N` neighbouring results of a right-hand side, alpha times the sums plus beta C.
 template <int N, bool BF16>
-__device__ __forceinline__ void put_some(const MxArgs& o, int64_t i, int64_t j, float (&v)[N]) {
+__device__ __forceinline__ void put_some(const MxArgs& o, int64_t i, int64_t j, const float (&v)[N]) {
     typedef float wide_t __attribute__((ext_vector_type(N)));
     typedef wide_t wide_f __attribute__((aligned(4)));
     typedef uint16_t half_t __attribute__((ext_vector_type(N)));
@@ -97,31 +97,49 @@ __device__ __forceinline__ void put_some(const MxArgs& o, int64_t i, int64_t j, 
     }
 }
 
-// A lane's results: right-hand side 32 x + l31 of its wave's, results (8 a + 4 h + b) TJ + y.
+// A wave's results.  A lane has results (8 a + 4 h + b) TJ + y of right-hand side 32 x + l31; they change places in
+// `room` (16 TJ x 256 bytes of this wave's), pieces of 16 bytes exchanged by the row, so that a store takes whole runs
+// of rows.
 template <int TI, int TJ, int WI, bool BF16>
-__device__ __forceinline__ void put_results(const MxArgs& o, int64_t i0, int64_t j0, const f32x4_t (&acc)[TI][TJ][4]) {
-    constexpr int N = TJ == 1 ? 4 : 8;   // at a time
+__device__ __forceinline__ void put_results(const MxArgs& o, int64_t i0, int64_t j0, const f32x4_t (&acc)[TI][TJ][4], char* room) {
+    constexpr int kRow = 128 * TJ, kPieces = kRow / 16;   // bytes and pieces of a row
+    constexpr int N = BF16 ? 8 : 4, kLanes = 32 * TJ / N; // results of a lane at a time, and lanes on a row
     const int lane = threadIdx.x & 63, l31 = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t i1 = i0 + wave % WI * TI * 32 + l31, j1 = j0 + wave / WI * TJ * 32;
+    const int64_t i1 = i0 + wave % WI * TI * 32, j1 = j0 + wave / WI * TJ * 32;
     const bool whole = j1 + 32 * TJ <= o.q;   // the same for the wave
 #pragma unroll
     for (int x = 0; x < TI; ++x) {
-        const int64_t i = i1 + 32 * x;
-        if (i >= o.s) continue;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-        for (int k = 0; k < 16 * TJ / N; ++k) {
-            const int a = k * N / (4 * TJ), in = k * N % (4 * TJ);
-            const int64_t j = j1 + (8 * a + 4 * h) * TJ + in;
+        for (int a = 0; a < 4; ++a)
+#pragma unroll
+            for (int k = 0; k < TJ; ++k) {
+                f32x4_t v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[x][(4 * k + e) % TJ][a][(4 * k + e) / TJ];
+                const int piece = (2 * a + h) * TJ + k;
+                *reinterpret_cast<f32x4_t*>(room + l31 * kRow + ((piece ^ l31) & (kPieces - 1)) * 16) = v;
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int k = 0; k < kLanes / 2; ++k) {
+            const int row = k * (64 / kLanes) + lane / kLanes, at = lane % kLanes * N;
             float v[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[e] = acc[x][(in + e) % TJ][a][(in + e) / TJ];
+            for (int e = 0; e < N; e += 4) {
+                const f32x4_t w = *reinterpret_cast<const f32x4_t*>(room + row * kRow + (((at + e) / 4 ^ row) & (kPieces - 1)) * 16);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[e + c] = w[c];
+            }
+            const int64_t i = i1 + 32 * x + row, j = j1 + at;
+            if (i >= o.s) continue;
             if (whole) {
                 put_some<N, BF16>(o, i, j, v);
             } else {
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    float u[1] = {v[e]};
+                    const float u[1] = {v[e]};
                     if (j + e < o.q) put_some<1, BF16>(o, i, j + e, u);
                 }
             }
@@ -148,7 +166,9 @@ template <int TI, int TJ, int WI, bool ACC, int MODE>
 __global__ __launch_bounds__(kThreads, 2) void f8_tile_kernel(TileArgs g) {
     constexpr int WJ = 8 / WI, BI = 32 * TI * WI, BJ = 32 * TJ * WJ, kRows = BI + BJ;
     constexpr int kLoads = kRows / 64;   // of 1 KB, eight rows, a wave has of a step
+    constexpr int kLoading = TJ == 4 ? 5 : TJ == 2 ? 3 : 2;   // half blocks of a tile row whose products they go out between
     static_assert(kRows % 64 == 0 && kRows <= kThreads, "rows must split evenly over the waves");
+    static_assert(4 * 4096 * TJ <= kRows * kF8Block, "a half of shared memory must hold four waves' results");
     static_assert(MODE != 0 || 128 % (32 * TJ) == 0, "a wave's results must lie in a block");
     static_assert(MODE != 1 || 128 % (32 * TI) == 0, "a wave's right-hand sides must lie in a block");
     // Two halves, of one step's codes and then scales each: two arrays, so that reads of one do not wait for what is
@@ -185,24 +205,33 @@ __global__ __launch_bounds__(kThreads, 2) void f8_tile_kernel(TileArgs g) {
     const float* s_base = s_of_p ? P.scales + t0 * P.lds + (i0 >> p_log) : Q.scales + t0 * Q.lds + (j0 >> q_log);
     const int64_t s_step = s_of_p ? P.lds : Q.lds;
     int64_t steps = t1 - t0, ahead = steps;   // of them not fetched yet
-    const auto fetch = [&](char* half) {
-        const Window p(p_base, 0xFFFFFFFF), q(q_base, 0xFFFFFFFF), sc(s_base, 0xFFFFFFFF);
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) {
+    // Load l of a step (the last one: its scales), and on to the next step.
+    const auto load = [&](char* half, int l) {
+        if (l < kLoads) {
             const int at = (wave * kLoads + l) * 8;
-            sixteen_to_shared(at < BI ? p : q, half + at * kF8Block, from[l]);
+            sixteen_to_shared(Window(at < BI ? p_base : q_base, 0xFFFFFFFF), half + at * kF8Block, from[l]);
+        } else {
+            four_to_shared(Window(s_base, 0xFFFFFFFF), half + kRows * kF8Block + wave * 256, s_from);
         }
-        four_to_shared(sc, half + kRows * kF8Block + wave * 256, s_from);
+    };
+    const auto advance = [&] {
         if (--ahead <= 0) return;   // the last step is fetched again: loads under a condition would be waited for at once
         p_base += kF8Block;
         q_base += kF8Block;
         s_base += s_step;
     };
+    const auto fetch = [&](char* half) {
+#pragma unroll
+        for (int l = 0; l <= kLoads; ++l) load(half, l);
+        advance();
+    };
 
     f32x4_t acc[TI][TJ][4] = {};
     // One step.  Pieces of a row lie exchanged by the row's place, (at >> 1) & 7: the 16-byte reads of sixteen lanes
     // together, eight pairs of rows, fill all banks.  This lane's pieces of a row are 2 h and 2 h + 1 of either half.
-    const auto multiply = [&](const char* half) {
+    // The next step's loads go out between the matrix instructions: at once, they would hold up the first of those.
+    const auto multiply = [&](const char* half, char* other) {
+        constexpr int kEach = (kLoads + 1 + kLoading - 1) / kLoading;
         const float* const sp = reinterpret_cast<const float*>(half + kRows * kF8Block) + wi;
         const float* const sq = reinterpret_cast<const float*>(half + kRows * kF8Block) + BI + wj;
         int own = l31 * kF8Block + (((2 * h) ^ (l31 >> 1)) & 7) * 16;
@@ -285,7 +314,13 @@ __global__ __launch_bounds__(kThreads, 2) void f8_tile_kernel(TileArgs g) {
                 }
             }
             if (u == 0) scales_of(y);
+            if (m < kLoading) {
+#pragma unroll
+                for (int l = m * kEach; l < (m + 1) * kEach && l <= kLoads; ++l) load(other, l);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
+        advance();
 #pragma unroll
         for (int x = 0; x < TI; ++x) add(x, TJ - 1, t[x]);
     };
@@ -301,22 +336,21 @@ __global__ __launch_bounds__(kThreads, 2) void f8_tile_kernel(TileArgs g) {
     if (steps & 1) {   // an odd number: one by itself, so that the loop has one way out
         fetch(half1);
         meet();
-        fetch(half0);
-        multiply(half1);
+        multiply(half1, half0);
     } else if (steps) {
         fetch(half0);
     }
     for (steps &= ~int64_t(1); steps > 0; steps -= 2) {
         meet();
-        fetch(half1);
-        multiply(half0);
+        multiply(half0, half1);
         meet();
-        fetch(half0);
-        multiply(half1);
+        multiply(half1, half0);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // shared memory is another workgroup's after this one
     if (place.split < 0) {
-        put_results<TI, TJ, WI, !ACC>(o, i0, j0, acc);
+        __syncthreads();   // every wave has read its operands: their place is taken
+        constexpr int kRoom = 4096 * TJ;   // a wave's
+        put_results<TI, TJ, WI, !ACC>(o, i0, j0, acc, wave < 4 ? half0 + wave * kRoom : half1 + (wave - 4) * kRoom);
     } else {
         float* const part = g.part + (place.split * g.cut.rest() + place.shared) * (BI * BJ);
 #pragma unroll
@@ -335,7 +369,8 @@ __global__ __launch_bounds__(kThreads) void f8_shared_kernel(TileArgs g) {
 #pragma unroll
         for (int n = 0; n < 4 * TI * TJ; ++n) acc[n / (4 * TJ)][n / 4 % TJ][n % 4] += *reinterpret_cast<const f32x4_t*>(part + (n * kThreads + threadIdx.x) * 4);
     }
-    put_results<TI, TJ, WI, BF16>(g.a.o, p.i * BI, p.j * BJ, acc);
+    __shared__ __attribute__((aligned(16))) char room[8 * 4096 * TJ];
+    put_results<TI, TJ, WI, BF16>(g.a.o, p.i * BI, p.j * BJ, acc, room + (threadIdx.x >> 6) * 4096 * TJ);
 }
 
 // Large tiles: 256 x 256 on the 8-bit instruction, 128 x 256 by way of bf16; else 64 x 128.
