@@ -248,9 +248,10 @@ __global__ __launch_bounds__(kThreads, 2) void f8_tile_kernel(TileArgs g) {
                     if constexpr (MODE == 1) by[a] *= one;
                 }
         };
-        const auto add = [&](int x, int y, const f32x16_t& v) {
+        // quarters a0 .. a1 - 1 of a tile's products, by their scales, to its sums
+        const auto add = [&](int x, int y, const f32x16_t& v, int a0, int a1) {
 #pragma unroll
-            for (int a = 0; a < 4; ++a) {
+            for (int a = a0; a < a1; ++a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float w = v[4 * a + e];
@@ -275,14 +276,20 @@ __global__ __launch_bounds__(kThreads, 2) void f8_tile_kernel(TileArgs g) {
 #pragma unroll
             for (int x = 0; x < TI; ++x) f[x] *= one;
         }
-        [[maybe_unused]] bf16x8 pv[TI][8];
-        if constexpr (ACC)
-#pragma unroll
-            for (int x = 0; x < TI; ++x)
-#pragma unroll
-                for (int u = 0; u < 8; ++u) pv[x][u] = f8_to_bf16(pw[x][u / 2][u % 2 * 2], pw[x][u / 2][u % 2 * 2 + 1]);
         const f32x16_t zero = {};
-        f32x16_t t[TI];
+        f32x16_t t[ACC && TJ > 1 ? 2 : 1][TI];
+        // ACC: operand `u` of a row, eight of its codes, as bf16.
+        const auto convert = [&](const u32x4_t& w, int u) {
+            u32x4_t v = __builtin_bit_cast(u32x4_t, f8_to_bf16(w[u % 2 * 2], w[u % 2 * 2 + 1]));
+            asm volatile("" : "+v"(v));   // between the matrix instructions, not before them
+            return __builtin_bit_cast(bf16x8, v);
+        };
+        [[maybe_unused]] bf16x8 pv[TI][8], qv[2];
+        if constexpr (ACC) {
+            qv[0] = convert(qw[0][0], 0);
+#pragma unroll
+            for (int x = 0; x < TI; ++x) pv[x][0] = convert(pw[x][0], 0);
+        }
 #pragma unroll
         for (int m = 0; m < 2 * TJ; ++m) {   // tile row m / 2, half m % 2 of the block
             const int y = m / 2, u = m % 2;
@@ -291,14 +298,20 @@ __global__ __launch_bounds__(kThreads, 2) void f8_tile_kernel(TileArgs g) {
                 qw[(m + 1) & 1][1] = piece(BI + wj + 32 * ((m + 1) / 2), (m + 1) % 2 * 2 + 1);
             }
             if constexpr (ACC) {
+                // Beside each pair of instructions: the next operands' conversion, and an eighth of the tile row before.
+                f32x16_t* const now = t[TJ > 1 ? y & 1 : 0];
+                f32x16_t* const last = t[TJ > 1 ? (y + 1) & 1 : 0];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const bf16x8 qv = f8_to_bf16(qw[u][k / 2][k % 2 * 2], qw[u][k / 2][k % 2 * 2 + 1]);
+                for (int k = 4 * u; k < 4 * u + 4; ++k) {
 #pragma unroll
                     for (int x = 0; x < TI; ++x) {
-                        if (m > 0 && u == 0 && k == 0) add(x, y - 1, t[x]);
-                        t[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qv, pv[x][4 * u + k], u + k ? t[x] : zero, 0, 0, 0);
-                        asm volatile("" : "+v"(t[x]));
+                        now[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qv[k & 1], pv[x][k], k ? now[x] : zero, 0, 0, 0);
+                        asm volatile("" : "+v"(now[x]));
+                        __builtin_amdgcn_sched_barrier(0);
+                        if (x == 0 && k + 1 < 4 * u + 4) qv[(k + 1) & 1] = convert(qw[u][(k + 1) % 4 / 2], k + 1);
+                        if (x == 0 && k + 1 == 4 * u + 4 && m + 1 < 2 * TJ) qv[(k + 1) & 1] = convert(qw[(m + 1) & 1][0], 0);
+                        if (y == 0 && k + 1 < 8) pv[x][k + 1] = convert(pw[x][(k + 1) / 2], k + 1);
+                        if (y > 0 && k % 2 == 0) add(x, y - 1, last[x], k / 2, k / 2 + 1);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
@@ -307,13 +320,14 @@ __global__ __launch_bounds__(kThreads, 2) void f8_tile_kernel(TileArgs g) {
 #pragma unroll
                 for (int x = 0; x < TI; ++x) {
                     const i32x8_t po = __builtin_bit_cast(i32x8_t, __builtin_shufflevector(pw[x][2 * u], pw[x][2 * u + 1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    if (m > 0 && u == 0) add(x, y - 1, t[x]);
-                    t[x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(qo, po, u ? t[x] : zero, 0, 0, 0, 0, 0, 0);
-                    asm volatile("" : "+v"(t[x]));
+                    if (m > 0 && u == 0) add(x, y - 1, t[0][x], 0, 4);
+                    t[0][x] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(qo, po, u ? t[0][x] : zero, 0, 0, 0, 0, 0, 0);
+                    asm volatile("" : "+v"(t[0][x]));
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            if (u == 0) scales_of(y);
+            // of this tile row, once the one before has had its own
+            if (ACC ? u == 1 : u == 0) scales_of(y);
             if (m < kLoading) {
 #pragma unroll
                 for (int l = m * kEach; l < (m + 1) * kEach && l <= kLoads; ++l) load(other, l);
@@ -322,7 +336,7 @@ __global__ __launch_bounds__(kThreads, 2) void f8_tile_kernel(TileArgs g) {
         }
         advance();
 #pragma unroll
-        for (int x = 0; x < TI; ++x) add(x, TJ - 1, t[x]);
+        for (int x = 0; x < TI; ++x) add(x, TJ - 1, t[ACC && TJ > 1 ? (TJ - 1) & 1 : 0][x], 0, 4);
     };
     // What this wave loaded into shared memory is there, and every wave is here and has read what it wanted.
     const auto meet = [] {
