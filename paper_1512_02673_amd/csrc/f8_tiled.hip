@@ -97,51 +97,46 @@ __device__ __forceinline__ void put_some(const MxArgs& o, int64_t i, int64_t j, 
     }
 }
 
-// A wave's results.  A lane has results (8 a + 4 h + b) TJ + y of right-hand side 32 x + l31; they change places in
-// `room` (16 TJ x 256 bytes of this wave's), pieces of 16 bytes exchanged by the row, so that a store takes whole runs
-// of rows.
-template <int TI, int TJ, int WI, bool BF16>
-__device__ __forceinline__ void put_results(const MxArgs& o, int64_t i0, int64_t j0, const f32x4_t (&acc)[TI][TJ][4], char* room) {
+// Results of the 32 right-hand sides from i0 on, a wave's 32 TJ from j0 on.  A lane has results (8 a + 4 h + b) TJ + y of
+// right-hand side l31; they change places in `room` (4 TJ KB of this wave's), pieces of 16 bytes exchanged by the row,
+// so that a store takes whole runs of rows.
+template <int TJ, bool BF16>
+__device__ __forceinline__ void put_rows(const MxArgs& o, int64_t i0, int64_t j0, const f32x4_t (&acc)[TJ][4], char* room) {
     constexpr int kRow = 128 * TJ, kPieces = kRow / 16;   // bytes and pieces of a row
     constexpr int N = BF16 ? 8 : 4, kLanes = 32 * TJ / N; // results of a lane at a time, and lanes on a row
     const int lane = threadIdx.x & 63, l31 = lane & 31, h = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t i1 = i0 + wave % WI * TI * 32, j1 = j0 + wave / WI * TJ * 32;
-    const bool whole = j1 + 32 * TJ <= o.q;   // the same for the wave
+    const bool whole = j0 + 32 * TJ <= o.q;   // the same for the wave
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-    for (int x = 0; x < TI; ++x) {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int a = 0; a < 4; ++a)
 #pragma unroll
-        for (int a = 0; a < 4; ++a)
+        for (int k = 0; k < TJ; ++k) {
+            f32x4_t v;
 #pragma unroll
-            for (int k = 0; k < TJ; ++k) {
-                f32x4_t v;
+            for (int e = 0; e < 4; ++e) v[e] = acc[(4 * k + e) % TJ][a][(4 * k + e) / TJ];
+            const int piece = (2 * a + h) * TJ + k;
+            *reinterpret_cast<f32x4_t*>(room + l31 * kRow + ((piece ^ l31) & (kPieces - 1)) * 16) = v;
+        }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = acc[x][(4 * k + e) % TJ][a][(4 * k + e) / TJ];
-                const int piece = (2 * a + h) * TJ + k;
-                *reinterpret_cast<f32x4_t*>(room + l31 * kRow + ((piece ^ l31) & (kPieces - 1)) * 16) = v;
-            }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int k = 0; k < kLanes / 2; ++k) {
+        const int row = k * (64 / kLanes) + lane / kLanes, at = lane % kLanes * N;
+        float v[N];
 #pragma unroll
-        for (int k = 0; k < kLanes / 2; ++k) {
-            const int row = k * (64 / kLanes) + lane / kLanes, at = lane % kLanes * N;
-            float v[N];
+        for (int e = 0; e < N; e += 4) {
+            const f32x4_t w = *reinterpret_cast<const f32x4_t*>(room + row * kRow + (((at + e) / 4 ^ row) & (kPieces - 1)) * 16);
 #pragma unroll
-            for (int e = 0; e < N; e += 4) {
-                const f32x4_t w = *reinterpret_cast<const f32x4_t*>(room + row * kRow + (((at + e) / 4 ^ row) & (kPieces - 1)) * 16);
+            for (int c = 0; c < 4; ++c) v[e + c] = w[c];
+        }
+        const int64_t i = i0 + row, j = j0 + at;
+        if (i >= o.s) continue;
+        if (whole) {
+            put_some<N, BF16>(o, i, j, v);
+        } else {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) v[e + c] = w[c];
-            }
-            const int64_t i = i1 + 32 * x + row, j = j1 + at;
-            if (i >= o.s) continue;
-            if (whole) {
-                put_some<N, BF16>(o, i, j, v);
-            } else {
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float u[1] = {v[e]};
-                    if (j + e < o.q) put_some<1, BF16>(o, i, j + e, u);
-                }
+            for (int e = 0; e < N; ++e) {
+                const float u[1] = {v[e]};
+                if (j + e < o.q) put_some<1, BF16>(o, i, j + e, u);
             }
         }
     }
@@ -364,7 +359,9 @@ __global__ __launch_bounds__(kThreads, 2) void f8_tile_kernel(TileArgs g) {
     if (place.split < 0) {
         __syncthreads();   // every wave has read its operands: their place is taken
         constexpr int kRoom = 4096 * TJ;   // a wave's
-        put_results<TI, TJ, WI, !ACC>(o, i0, j0, acc, wave < 4 ? half0 + wave * kRoom : half1 + (wave - 4) * kRoom);
+        char* const room = wave < 4 ? half0 + wave * kRoom : half1 + (wave - 4) * kRoom;
+#pragma unroll
+        for (int x = 0; x < TI; ++x) put_rows<TJ, !ACC>(o, i0 + wi + 32 * x, j0 + wj, acc[x], room);
     } else {
         float* const part = g.part + (place.split * g.cut.rest() + place.shared) * (BI * BJ);
 #pragma unroll
@@ -372,22 +369,47 @@ __global__ __launch_bounds__(kThreads, 2) void f8_tile_kernel(TileArgs g) {
     }
 }
 
-// The shared tiles' results from the sums of their splits, added in order.
+// The shared tiles' results from the sums of their splits.  A workgroup takes 32 right-hand sides of one wave's results;
+// its four waves add up splits in turn, in order, and the first adds up theirs.
 template <int TI, int TJ, int WI, bool BF16>
-__global__ __launch_bounds__(kThreads) void f8_shared_kernel(TileArgs g) {
-    constexpr int BI = 32 * TI * WI, BJ = 32 * TJ * (8 / WI);
-    const Place p = place_of(g.cut, g.cut.whole + blockIdx.x);
-    f32x4_t acc[TI][TJ][4] = {};
-    for (int64_t k = 0; k < g.cut.splits; ++k) {
-        const float* const part = g.part + (k * g.cut.rest() + blockIdx.x) * (BI * BJ);
+__global__ __launch_bounds__(256) void f8_shared_kernel(TileArgs g) {
+    constexpr int BI = 32 * TI * WI, BJ = 32 * TJ * (8 / WI), kParts = 4 * TJ;
+    __shared__ __attribute__((aligned(16))) f32x4_t sums[4][kParts][64];
+    const int64_t tile = blockIdx.x / (8 * TI);
+    const int wave = blockIdx.x / TI % 8, x = blockIdx.x % TI, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    f32x4_t acc[TJ][4] = {};
+    for (int64_t k = w; k < g.cut.splits; k += 4) {
+        const float* const part = g.part + (k * g.cut.rest() + tile) * (BI * BJ) + ((x * kParts * 8 + wave) * 64 + lane) * 4;
 #pragma unroll
-        for (int n = 0; n < 4 * TI * TJ; ++n) acc[n / (4 * TJ)][n / 4 % TJ][n % 4] += *reinterpret_cast<const f32x4_t*>(part + (n * kThreads + threadIdx.x) * 4);
+        for (int n = 0; n < kParts; ++n) acc[n / 4][n % 4] += *reinterpret_cast<const f32x4_t*>(part + n * kThreads * 4);
     }
-    __shared__ __attribute__((aligned(16))) char room[8 * 4096 * TJ];
-    put_results<TI, TJ, WI, BF16>(g.a.o, p.i * BI, p.j * BJ, acc, room + (threadIdx.x >> 6) * 4096 * TJ);
+#pragma unroll
+    for (int n = 0; n < kParts; ++n) sums[w][n][lane] = acc[n / 4][n % 4];
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int n = 0; n < kParts; ++n)
+#pragma unroll
+        for (int k = 1; k < 4; ++k) acc[n / 4][n % 4] += sums[k][n][lane];
+    const Place p = place_of(g.cut, g.cut.whole + tile);
+    put_rows<TJ, BF16>(g.a.o, p.i * BI + wave % WI * TI * 32 + 32 * x, p.j * BJ + wave / WI * TJ * 32, acc, reinterpret_cast<char*>(sums[0]));
 }
 
-// Large tiles: 256 x 256 on the 8-bit instruction, 128 x 256 by way of bf16; else 64 x 128.
+// Microseconds of one block in each of `groups` workgroups at once, as measured (4096 terms): up to one a compute unit,
+// and more, large ones in rounds.  `acc`: by way of bf16.
+double step_us(bool large, bool acc, int64_t groups) {
+    const double one = large ? (acc ? 1.4 : 1.15) : acc ? 0.6 : 0.33, full = large ? (acc ? 1.85 : 1.7) : acc ? 0.85 : 0.53;
+    if (groups <= 256) return one + (full - one) * groups / 256;
+    if (large) return full * ceil_div(groups, 256);
+    return (acc ? 1.33 : 0.74) * (groups <= 512 ? 1.0 : groups / 512.0);
+}
+// Large tiles (256 x 256 on the 8-bit instruction, 128 x 256 by way of bf16) or small ones (64 x 128), and into how many
+// splits what is left over from whole rounds of large tiles, or a product of less than a round, is cut: by the least
+// estimated time.  A large tile's beginning and end take 8 us, a small one's 5; splits' sums 5 us and 0.35 for each MB of
+// them.  Measured (large tiles with 1 to 16 splits; small ones), us, bf16 results of 4096 terms, side by side:
+// 512 x 512 45 30 22 20 23; 16 13 12 14 16, 1024 x 1024 46 32 25 25 32; 17 19 18 23 32, 2048 x 2048 47 49 51 72; 28 43 47 64,
+// 4096 x 4096 64 142; 102 174, 16384 x 100 45 47 48 67; 25 29 34 46; of 16384, 1000 x 1000 164 93 57 42 44; 76 50 39 43 49;
+// fp32 results, 512 x 512 54 33 22 19 20; 24 18 14 15 17, 4096 x 4096 135 176; 178 228.
 Cut cut_of(const F8Args& a) {
     const bool acc = !a.o.y_bf16;
     Cut best{};
@@ -398,15 +420,17 @@ Cut cut_of(const F8Args& a) {
         c.bj = large ? 256 : 128;
         c.tiles_i = ceil_div(a.o.s, c.bi);
         c.tiles_j = ceil_div(a.o.q, c.bj);
-        const double step = large ? 2.0 : 1.0;   // us of a block
-        const int64_t round = large ? 256 : 512, tiles = c.tiles_i * c.tiles_j, whole = tiles / round * round;
+        const double edge = large ? 8 : 5;
+        const int64_t tiles = c.tiles_i * c.tiles_j, whole = large ? tiles / 256 * 256 : 0, rest = tiles - whole;
         for (int64_t splits = 1; splits <= 64; splits *= 2) {
-            if (splits > 1 && (splits > a.blocks / 2 || (tiles - whole) * splits > 2 * round)) break;
+            if (splits > 1 && (splits > a.blocks / 2 || rest == 0 || rest * splits > 2048)) break;
             c.whole = splits > 1 ? whole : tiles;
             c.per = std::max<int64_t>(1, ceil_div(a.blocks, splits));
             c.splits = splits > 1 ? ceil_div(a.blocks, c.per) : 1;
-            double us = (whole / round * a.blocks + ceil_div((tiles - whole) * c.splits, round) * c.per) * step;
-            if (c.splits > 1) us += 5 + c.part_bytes() * 2 / 4e6;
+            const int64_t groups = rest * c.splits;
+            double us = whole / 256 * (a.blocks * step_us(large, acc, 256) + edge);
+            if (groups > 0) us += c.per * step_us(large, acc, groups) + edge * (large ? ceil_div(groups, 256) : std::max(1.0, groups / 512.0));
+            if (c.splits > 1) us += 5 + 0.35e-6 * c.part_bytes();
             if (best_us < 0 || us < best_us) {
                 best_us = us;
                 best = c;
@@ -431,8 +455,9 @@ hipError_t launch_tiles(TileArgs g, hipStream_t st) {
         if (e != hipSuccess) return e;
     }
     if (g.cut.splits <= 1) return hipSuccess;
-    if (!grid_fits(g.cut.rest(), kThreads)) return hipErrorInvalidConfiguration;
-    f8_shared_kernel<TI, TJ, WI, !ACC><<<dim3(static_cast<uint32_t>(g.cut.rest())), kThreads, 0, st>>>(g);
+    const int64_t joins = g.cut.rest() * 8 * TI;
+    if (!grid_fits(joins, 256)) return hipErrorInvalidConfiguration;
+    f8_shared_kernel<TI, TJ, WI, !ACC><<<dim3(static_cast<uint32_t>(joins)), 256, 0, st>>>(g);
     return hipGetLastError();
 }
 
