@@ -17,7 +17,7 @@
 #include <algorithm>
 
 #include "f8.h"
-#include "rows.h"
+#include "to_shared.h"
 
 namespace coded {
 namespace {
@@ -140,18 +140,6 @@ __device__ __forceinline__ void put_rows(const MxArgs& o, int64_t i0, int64_t j0
             }
         }
     }
-}
-
-// 16 or 4 bytes a lane from `from` bytes on, to `to` in shared memory (the wave's first lane's; the others' follow).
-__device__ __forceinline__ void sixteen_to_shared(const Window& w, char* to, uint32_t from) {
-#ifdef __HIP_DEVICE_COMPILE__   // the host's pass knows no such load, and would drop the kernel
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(w.rsrc, (__attribute__((address_space(3))) void*)to, 16, from, 0, 0, 0);
-#endif
-}
-__device__ __forceinline__ void four_to_shared(const Window& w, char* to, uint32_t from) {
-#ifdef __HIP_DEVICE_COMPILE__
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(w.rsrc, (__attribute__((address_space(3))) void*)to, 4, from, 0, 0, 0);
-#endif
 }
 
 // TI x TJ tiles of 32 x 32 a wave, WI waves along the right-hand sides and 8 / WI along the results.  ACC: by way of
