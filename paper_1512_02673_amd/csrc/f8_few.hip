@@ -1,13 +1,22 @@
-// Products of 8-bit matrices, results 16 rows of Q at a time: out[i][j] = sum over
-// blocks b of sP[b][i] sQ[b][j] (sum over b's columns of P[i][k] Q[j][k]).
+// Products of 8-bit matrices with few right-hand sides: out[i][j] = sum over blocks b of
+// sP[b][i] sQ[b][j] (sum over b's columns of P[i][k] Q[j][k]).
 //
-// Codes become bf16 values in registers, which is exact, and meet on the bf16
-// matrix instructions, whose products and sums are in fp32.  A workgroup takes 16
-// results of 16 NT right-hand sides; its four waves take blocks in turn and add
-// their sums up in shared memory.  Lane (li, lk) of a block holds columns 16 lk ..
-// 16 lk + 15 and 64 more of row li, so a load takes 64 bytes of each row.
-// Where there are few workgroups the blocks are split among several, whose sums
-// are joined in order.
+// Bound: reading Q's codes.  A workgroup takes 16 results, or 32 where that leaves
+// two workgroups a compute unit, of all right-hand sides; its four waves take every
+// fourth block each and add their sums up in shared memory.  Each wave has a room of
+// its own there for three blocks' codes, two of them on their way, in loads of whole
+// rows of a block; no wave waits for another.  Codes become bf16 values in
+// registers, which is exact, and meet on the bf16 matrix instructions, whose
+// products and sums are in fp32, for results of either type.  Where there are few
+// workgroups the blocks are split among several, whose sums are joined in order.
+//
+// Measured, us: 65536 x 8192 times 1 and 16: 93 and 100 (5.8 and 5.4 TB/s; loads in
+// the operands' order, half rows, into registers 118 and 126, without non-temporal
+// loads 102 and 108, with workgroups in turn instead of runs of them on the XCDs 124
+// and 122), 16384 x 4096 times 1 and 32: 13 and 16, 11500 x 5750 times 16: 13.  Small
+// tiles (f8_tiled.hip) with up to 64 right-hand sides take 90 (fp32 results 115), 24
+// (23) and 22 (28): so from 33 on, or from 17 on where the codes do not stay in the
+// memory-side cache.
 #include <algorithm>
 #include <utility>
 
@@ -34,8 +43,8 @@ __device__ __forceinline__ void to_operands(const u32x4_t (&w)[2], bf16x8 (&v)[4
     }
 }
 
-// 8 PE right-hand sides, RT tiles of 16 results.  QB: Q's scales are for 128 rows.
-template <int PE, int RT, bool QB>
+// 8 PE right-hand sides, RT tiles of 16 results.  QB: Q's scales are for 128 rows.  NTL: non-temporal loads of Q.
+template <int PE, int RT, bool QB, bool NTL>
 __global__ __launch_bounds__(kThreads) void f8_few_kernel(FewArgs g) {
     constexpr int NT = (PE + 1) / 2, kQ = RT * 2048, kStage = kQ + NT * 2048;
     // Three steps of each wave's: three arrays, so that reads of one do not wait for what is on its way into another.
@@ -47,7 +56,9 @@ __global__ __launch_bounds__(kThreads) void f8_few_kernel(FewArgs g) {
     const MxArgs& o = g.a.o;
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lk = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t id = g.first + blockIdx.x, split = id / g.groups;
+    // Workgroups go to the eight XCDs in turn: each takes a run of them.
+    const int64_t base = gridDim.x / 8, more = gridDim.x % 8, xcd = blockIdx.x % 8;
+    const int64_t id = g.first + xcd * base + lesser(xcd, more) + blockIdx.x / 8, split = id / g.groups;
     const int64_t j0 = id % g.groups * 16 * RT, n = o.q;
     const int s = static_cast<int>(o.s);
     // Load l of a matrix takes rows 8 l .. 8 l + 7, whole blocks of 128 bytes; pieces of 16 bytes lie exchanged by
@@ -82,7 +93,7 @@ __global__ __launch_bounds__(kThreads) void f8_few_kernel(FewArgs g) {
         const int64_t at = b0 + 4 * (there ? k : steps - 1);   // past the last step: that one again, times zero
         const Window q(Q.codes + j0 * Q.ldc + at * kF8Block, 0xFFFFFFFF), p(P.codes + at * kF8Block, 0xFFFFFFFF);
 #pragma unroll
-        for (int l = 0; l < 2 * RT; ++l) sixteen_to_shared(q, to + l * 1024, q_from[l]);
+        for (int l = 0; l < 2 * RT; ++l) sixteen_to_shared<NTL>(q, to + l * 1024, q_from[l]);
 #pragma unroll
         for (int l = 0; l < PE; ++l) sixteen_to_shared(p, to + kQ + l * 1024, p_from[l]);
         const Window sp(P.scales + at * P.lds, 0xFFFFFFFF);
@@ -178,7 +189,9 @@ Plan plan_of(const F8Args& a) {
 
 template <int PE, int RT>
 hipError_t launch_one(const FewArgs& g, int64_t groups, hipStream_t st) {
-    const auto kernel = g.a.Q.block_rows != 1 ? f8_few_kernel<PE, RT, true> : f8_few_kernel<PE, RT, false>;
+    const bool ntl = streams(g.a.o.q * g.a.blocks * kF8Block);
+    const auto kernel = g.a.Q.block_rows != 1 ? (ntl ? f8_few_kernel<PE, RT, true, true> : f8_few_kernel<PE, RT, true, false>)
+                                              : (ntl ? f8_few_kernel<PE, RT, false, true> : f8_few_kernel<PE, RT, false, false>);
     kernel<<<dim3(static_cast<uint32_t>(groups)), kThreads, 0, st>>>(g);
     return hipGetLastError();
 }
@@ -190,7 +203,7 @@ hipError_t launch_rows(const FewArgs& g, int rt, int64_t groups, hipStream_t st)
 
 }  // namespace
 
-bool f8_few_serves(const F8Args& a) { return a.o.s <= 32; }
+bool f8_few_serves(const F8Args& a) { return a.o.s <= (streams(a.o.q * a.blocks * kF8Block) ? 16 : 32); }
 
 int64_t f8_few_workspace_bytes(const F8Args& a) {
     const Plan p = plan_of(a);
@@ -209,16 +222,15 @@ hipError_t launch_f8_few(const F8Args& a, hipStream_t st) {
     return p.splits > 1 ? launch_mx_join(a.o, g.part, p.splits, a.o.q, st) : hipSuccess;
 }
 
-// The sides change places where Y has the other order: the tiles write rows of it, and few results of many
-// right-hand sides are few right-hand sides with many results.
+// The sides change places where few results of many right-hand sides are few right-hand sides with many results, and
+// where Y has the other order: the tiles write rows of it.
 static F8Args arranged(F8Args a) {
-    const bool turn = f8_few_serves(a) ? false : a.o.q <= 32 ? true : !a.o.y_rows;
-    if (turn) {
-        std::swap(a.P, a.Q);
-        std::swap(a.o.q, a.o.s);
-        a.o.y_rows = !a.o.y_rows;
-    }
-    return a;
+    if (f8_few_serves(a)) return a;
+    F8Args other = a;
+    std::swap(other.P, other.Q);
+    std::swap(other.o.q, other.o.s);
+    other.o.y_rows = !a.o.y_rows;
+    return f8_few_serves(other) || !a.o.y_rows ? other : a;
 }
 
 int64_t f8_workspace_bytes(const F8Args& given) {
