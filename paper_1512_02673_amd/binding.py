@@ -734,14 +734,18 @@ def coded_mx_mm_t(M: MXMatrix, U, Z, x_rows: bool = False, y_rows: bool = False,
 
 # ---------------------------------------------------------------- matrices in 8 bits, dropout, embeddings
 
-def _on_gpu(*named):
-    """Every tensor must be in the current device's memory: another device's, or the host's, would fault there."""
-    for name, t in named:
-        if t is not None and not t.is_cuda:
+def _on_gpu(names, tensors):
+    """Every tensor (None: left out) must be in the current device's memory: another device's, or the host's, would fault."""
+    device = -2
+    for name, t in zip(names, tensors):
+        if t is None:
+            continue
+        at = t.get_device()      # -1: the host
+        if at < 0:
             raise ValueError(f"{name} must be on the GPU")
-    device = _torch().cuda.current_device()
-    for name, t in named:
-        if t is not None and t.get_device() != device:
+        if device == -2:
+            device = _torch().cuda.current_device()
+        if at != device:
             raise ValueError(f"{name} must be on the current device, {device}")
 
 
@@ -763,16 +767,21 @@ class F8Matrix:
         torch = _torch()
         if block_rows not in (1, 128):
             raise ValueError("a block must have 1 or 128 rows")
-        width, blocks, groups = (cols + 127) // 128 * 128, (cols + 127) // 128, (rows + block_rows - 1) // block_rows
+        blocks, groups = (cols + 127) // 128, (rows + block_rows - 1) // block_rows
+        width = blocks * 128
         if codes.dtype is not torch.uint8 or scales.dtype is not torch.float32 or codes.dim() != 2 or scales.dim() != 2:
             raise ValueError("codes must be uint8 and scales float32, both 2-D")
-        if rows < 0 or cols < 0 or codes.shape[0] != rows or codes.shape[1] < width or (width and codes.stride(1) != 1):
+        n, wide = codes.shape
+        n_s, wide_s = scales.shape
+        ldc, step = codes.stride()
+        lds, step_s = scales.stride()
+        if rows < 0 or cols < 0 or n != rows or wide < width or (width and step != 1):
             raise ValueError(f"codes must be {rows} rows of at least {width} bytes")
-        if scales.shape[0] < blocks or scales.shape[1] < groups or (groups > 1 and scales.stride(1) != 1):
+        if n_s < blocks or wide_s < groups or (groups > 1 and step_s != 1):
             raise ValueError(f"scales must be {blocks} rows of at least {groups} elements")
         self.codes, self.scales, self.rows_, self.cols, self.block_rows = codes, scales, rows, cols, block_rows
-        self.ldc = codes.stride(0) if rows > 1 and cols > 0 else width
-        self.lds = scales.stride(0) if blocks > 1 else groups
+        self.ldc = ldc if rows > 1 and cols > 0 else width
+        self.lds = lds if blocks > 1 else groups
 
     @property
     def shape(self):
@@ -802,8 +811,12 @@ def alloc_f8(q: int, r: int, block_rows: int = 1, device="cuda") -> F8Matrix:
     if q < 0 or r < 0 or block_rows not in (1, 128):
         raise ValueError("sizes must be >= 0 and a block have 1 or 128 rows")
     blocks = (r + 127) // 128
-    return F8Matrix(torch.empty((q, blocks * 128), dtype=torch.uint8, device=device),
-                    torch.empty((blocks, (q + block_rows - 1) // block_rows), dtype=torch.float32, device=device), q, r, block_rows)
+    width, groups = blocks * 128, (q + block_rows - 1) // block_rows
+    M = F8Matrix.__new__(F8Matrix)      # what its checks would find is known
+    M.codes = torch.empty((q, width), dtype=torch.uint8, device=device)
+    M.scales = torch.empty((blocks, groups), dtype=torch.float32, device=device)
+    M.rows_, M.cols, M.block_rows, M.ldc, M.lds = q, r, block_rows, width, groups
+    return M
 
 
 def coded_f8_quantize(A, M: "F8Matrix | None" = None, MT: "F8Matrix | None" = None, stream=None) -> None:
@@ -815,7 +828,8 @@ def coded_f8_quantize(A, M: "F8Matrix | None" = None, MT: "F8Matrix | None" = No
         raise ValueError("M must have A's shape")
     if MT is not None and MT.shape != (r, q):
         raise ValueError("MT must have the shape of A's transpose")
-    _on_gpu(("A", A), *((n, t) for n, m in (("M", M), ("MT", MT)) if m is not None for t in (m.codes, m.scales)))
+    _on_gpu(("A", "M", "M", "MT", "MT"), (A, *((None, None) if M is None else (M.codes, M.scales)),
+                                          *((None, None) if MT is None else (MT.codes, MT.scales))))
     none = 1, None, 0, None, 0
     _check(lib().coded_f8_quantize(dt, A.data_ptr(), q, r, lda, *(none if M is None else M._args()),
                                    *(none if MT is None else MT._args()), _stream(stream)))
@@ -826,7 +840,7 @@ def coded_f8_dequantize(M: F8Matrix, out, stream=None) -> None:
     q, r, ldo, dt = _mx_dense(out, "out")
     if M.shape != (q, r):
         raise ValueError("out must have M's shape")
-    _on_gpu(("out", out), ("M", M.codes), ("M", M.scales))
+    _on_gpu(("out", "M", "M"), (out, M.codes, M.scales))
     _check(lib().coded_f8_dequantize(q, r, *M._args(), dt, out.data_ptr(), ldo, _stream(stream)))
 
 
@@ -860,8 +874,8 @@ def coded_f8_mm(A: F8Matrix, X: F8Matrix, Y, y_rows: bool = False, alpha: float 
         else:
             raise ValueError("C must have Y's shape, or be one row of it")
         cp = C.data_ptr()
-    _on_gpu(("Y", Y), ("A", A.codes), ("A", A.scales), ("X", X.codes), ("X", X.scales), ("C", C if beta != 0 else None),
-            ("workspace", None if isinstance(workspace, str) else workspace))
+    _on_gpu(("Y", "A", "A", "X", "X", "C", "workspace"), (Y, A.codes, A.scales, X.codes, X.scales, C if beta != 0 else None,
+                                                        None if isinstance(workspace, str) else workspace))
     wsp, wsb = None, 0
     if isinstance(workspace, str):
         wsb = coded_f8_workspace(q, r, s, y_dt, y_rows)
@@ -888,7 +902,7 @@ def coded_dropout(X, out, p: float, seed: int, draw: int, first_row: int = 0, C=
             raise ValueError("C must have X's shape and type")
     if not 0 <= seed < 1 << 64 or not 0 <= draw < 1 << 56:
         raise ValueError("seed must be in [0, 2^64) and draw in [0, 2^56)")
-    _on_gpu(("X", X), ("out", out), ("C", C))
+    _on_gpu(("X", "out", "C"), (X, out, C))
     _check(lib().coded_dropout(dt, X.data_ptr(), q, r, ldx, p, seed, draw, first_row, _ptr(C), ldcc, out.data_ptr(), ldo,
                                _stream(stream)))
 
@@ -908,7 +922,7 @@ def coded_embed(E, tok, out, scale: float = 1.0, skip: int = -1, stream=None) ->
     tp, size, n = _tokens(tok)
     if E.dim() != 2 or out.dim() != 2 or (n_out, d_out) != (n, d):
         raise ValueError(f"out must be {n} rows of {d}")
-    _on_gpu(("E", E), ("tok", tok), ("out", out))
+    _on_gpu(("E", "tok", "out"), (E, tok, out))
     _check(lib().coded_embed(e_dt, E.data_ptr(), vocab, d, lde, tp, size, n, skip, scale, out_dt, out.data_ptr(), ldo, _stream(stream)))
 
 
@@ -928,7 +942,7 @@ def coded_embed_grad(G, tok, dE, scale: float = 1.0, beta: float = 0.0, skip: in
     tp, size, n = _tokens(tok)
     if G.dim() != 2 or dE.dim() != 2 or (n_g, d_g) != (n, d):
         raise ValueError(f"G must be {n} rows of {d}")
-    _on_gpu(("G", G), ("tok", tok), ("dE", dE), ("workspace", None if isinstance(workspace, str) else workspace))
+    _on_gpu(("G", "tok", "dE", "workspace"), (G, tok, dE, None if isinstance(workspace, str) else workspace))
     wsp, wsb = None, 0
     if isinstance(workspace, str):
         wsb = coded_embed_workspace(n, vocab, d)

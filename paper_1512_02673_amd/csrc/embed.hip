@@ -56,6 +56,7 @@ __global__ __launch_bounds__(kThreads) void embed_count_kernel(const void* tok, 
     __shared__ int before[4][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int padded = (n + 15) / 16 * 16;
+#pragma unroll 4
     for (int i = tid; i < padded; i += kThreads) all[i] = i < n ? row_of<WIDE>(tok, i, vocab, skip) : 0xFFFFFFFFu;
     __syncthreads();
     const int i = blockIdx.x * 64 + lane;
@@ -213,7 +214,7 @@ __device__ __forceinline__ void put_row(const EmbedGradArgs& a, int64_t row, int
 
 // Rows without a token: zero, or beta times what they were.
 template <bool E16>
-__device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, const uint32_t* keys, const RunChunks& g, int64_t first) {
+__device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, const uint32_t* keys, const RunChunks& g, const RowCut& cut, int64_t first) {
     __shared__ uint32_t there[64];
     const int tid = threadIdx.x;
     if (tid < g.fill_rows) {
@@ -222,9 +223,27 @@ __device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, const uint32_t
         there[tid] = first + tid >= a.vocab || (at < g.n && keys[at] == row);
     }
     __syncthreads();
-    for (int64_t k = 0; k < g.fill_rows; ++k) {
+    constexpr int kSize = E16 ? 2 : 4, kEach = 16 / kSize;
+    if (a.beta == 0.0f) {   // 16 bytes a lane, lanes next to each other
+        const int lane = tid & 63;
+        for (int64_t k = tid >> 6; k < g.fill_rows; k += kThreads / 64) {
+            if (there[k]) continue;
+            char* const to = static_cast<char*>(a.dE) + (first + k) * a.ldde * kSize;
+            const int64_t whole = a.d / kEach;
+            for (int64_t c = lane; c < whole; c += 64) *reinterpret_cast<u32x4_bf*>(to + c * 16) = u32x4_t{0u, 0u, 0u, 0u};
+            for (int64_t c = whole * kEach + lane; c < a.d; c += 64) {
+                if constexpr (E16)
+                    reinterpret_cast<uint16_t*>(to)[c] = 0;
+                else
+                    reinterpret_cast<float*>(to)[c] = 0.0f;
+            }
+        }
+        return;
+    }
+    const int64_t c0 = (tid & ((1 << cut.log_tpr) - 1)) * 8;
+    for (int64_t k = tid >> cut.log_tpr; k < g.fill_rows; k += cut.rows(kThreads)) {
         if (there[k]) continue;
-        for (int64_t c = tid * 8; c < a.d; c += kThreads * 8) {
+        for (int64_t c = c0; c < a.d; c += int64_t(8) << cut.log_tpr) {
             float v[8] = {};
             put_row<E16>(a, first + k, c, v);
         }
@@ -236,11 +255,11 @@ __device__ __forceinline__ float* part_of(float* parts, int64_t chunk, int which
 template <bool G16, bool E16>
 __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedGradArgs a, const uint32_t* keys, const uint32_t* index, RunChunks g, RowCut cut,
                                                             float* parts) {
-    if (blockIdx.x < g.fills) {
-        fill_rows<E16>(a, keys, g, blockIdx.x * g.fill_rows);
+    const int64_t id = blockIdx.x, sums = gridDim.x - g.fills;
+    if (id >= sums) {
+        fill_rows<E16>(a, keys, g, cut, (id - sums) * g.fill_rows);
         return;
     }
-    const int64_t id = blockIdx.x - g.fills;
     const int64_t chunk = id / cut.pieces * cut.rows(kThreads) + (threadIdx.x >> cut.log_tpr);
     const int64_t c = ((id % cut.pieces << cut.log_tpr) + (threadIdx.x & ((1 << cut.log_tpr) - 1))) * 8;
     if (chunk >= g.count || c >= a.d) return;
@@ -260,21 +279,33 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedGradArgs a, co
         for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
         head = false;
     };
-    for (int64_t p = p0; p < p1; p += 4) {
-        float v[4][8];
-        uint32_t key[4];
+    // Rows in groups of kRows at once, and the next group's keys and places meanwhile; past the end the last one again.
+    constexpr int kRows = G16 ? 8 : 4;
+    uint32_t key[kRows], place[kRows];
+    const auto look = [&](int64_t p) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < kRows; ++e) {
             const int64_t at = lesser(p + e, p1 - 1);
             key[e] = keys[at];
-            row_load<G16>(static_cast<const char*>(a.G) + static_cast<int64_t>(index[at]) * a.ldg * (G16 ? 2 : 4), c, a.d, v[e]);
+            place[e] = index[at];
         }
+    };
+    look(p0);
+    for (int64_t p = p0; p < p1; p += kRows) {
+        float v[kRows][8];
+        uint32_t now[kRows];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < kRows; ++e) {
+            now[e] = key[e];
+            row_load<G16>(static_cast<const char*>(a.G) + static_cast<int64_t>(place[e]) * a.ldg * (G16 ? 2 : 4), c, a.d, v[e]);
+        }
+        look(p + kRows);
+#pragma unroll
+        for (int e = 0; e < kRows; ++e) {
             if (p + e >= p1) break;
-            if (key[e] != run) {
+            if (now[e] != run) {
                 end_run(false);
-                run = key[e];
+                run = now[e];
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) sum[k] += v[e][k];
@@ -299,7 +330,7 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedGradArgs a, c
     float sum[8] = {};
     if (c < a.d) {
         if (wave == 0) row_load<false>(part_of(parts, chunk, 1, a.d), c, a.d, sum);
-#pragma unroll 4
+#pragma unroll 8
         for (int64_t k = chunk + 1 + wave; k <= last; k += 4) {
             float v[8];
             row_load<false>(part_of(parts, k, 0, a.d), c, a.d, v);
@@ -331,7 +362,7 @@ Plan plan_of(int64_t n, int64_t vocab, int64_t d) {
     p.cut = cut_rows(d, kLogThreads);
     p.list = round_up(n * 4, 256);
     p.chunks.n = n;
-    p.chunks.per = std::min<int64_t>(32, std::max<int64_t>(8, n / 1024));
+    p.chunks.per = std::min<int64_t>(64, std::max<int64_t>(8, n / 1024));
     p.chunks.count = ceil_div(n, p.chunks.per);
     p.parts = round_up(p.chunks.count * 2 * d * 4, 256);
     return p;
@@ -381,7 +412,7 @@ hipError_t sum_rows(const EmbedGradArgs& a, Plan p, const uint32_t* keys, const 
     float* parts = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + 4 * p.list + kMostBlocks * kMostBins * 4);
     RunChunks& g = p.chunks;
     if (a.beta != 1.0f) {
-        g.fill_rows = std::min<int64_t>(64, std::max<int64_t>(1, (int64_t(1) << 15) / a.d));
+        g.fill_rows = std::min<int64_t>(64, std::max<int64_t>(1, a.vocab / 2048));
         g.fills = ceil_div(a.vocab, g.fill_rows);
     }
     const int64_t blocks = g.fills + ceil_div(g.count, p.cut.rows(kThreads)) * p.cut.pieces;
