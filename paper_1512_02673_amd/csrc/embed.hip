@@ -215,7 +215,7 @@ __device__ __forceinline__ void put_row(const EmbedGradArgs& a, int64_t row, int
 // Rows without a token: zero, or beta times what they were.
 template <bool E16>
 __device__ __forceinline__ void fill_rows(const EmbedGradArgs& a, const uint32_t* keys, const RunChunks& g, const RowCut& cut, int64_t first) {
-    __shared__ uint32_t there[64];
+    __shared__ uint32_t there[kThreads];
     const int tid = threadIdx.x;
     if (tid < g.fill_rows) {
         const uint32_t row = static_cast<uint32_t>(first + tid);
@@ -362,7 +362,7 @@ Plan plan_of(int64_t n, int64_t vocab, int64_t d) {
     p.cut = cut_rows(d, kLogThreads);
     p.list = round_up(n * 4, 256);
     p.chunks.n = n;
-    p.chunks.per = std::min<int64_t>(64, std::max<int64_t>(8, n / 1024));
+    p.chunks.per = std::max(std::min<int64_t>(64, std::max<int64_t>(8, n / 1024)), ceil_div(n, int64_t(1) << 20));
     p.chunks.count = ceil_div(n, p.chunks.per);
     p.parts = round_up(p.chunks.count * 2 * d * 4, 256);
     return p;
@@ -412,7 +412,7 @@ hipError_t sum_rows(const EmbedGradArgs& a, Plan p, const uint32_t* keys, const 
     float* parts = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + 4 * p.list + kMostBlocks * kMostBins * 4);
     RunChunks& g = p.chunks;
     if (a.beta != 1.0f) {
-        g.fill_rows = std::min<int64_t>(64, std::max<int64_t>(1, a.vocab / 2048));
+        g.fill_rows = std::min<int64_t>(kThreads, std::max<int64_t>(1, a.vocab / 2048));
         g.fills = ceil_div(a.vocab, g.fill_rows);
     }
     const int64_t blocks = g.fills + ceil_div(g.count, p.cut.rows(kThreads)) * p.cut.pieces;

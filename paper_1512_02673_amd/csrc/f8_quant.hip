@@ -192,7 +192,7 @@ hipError_t launch_f8_quantize(const void* A, bool bf16, int64_t q, int64_t r, in
 
 hipError_t launch_f8_dequantize(const F8Mat& m, int64_t r, void* out, bool bf16, int64_t ldo, hipStream_t st) {
     const RowCut cut = cut_rows(r, 8);
-    const int64_t step = kMostBlocks / cut.pieces * kF8Block;
+    const int64_t step = kMostBlocks / cut.pieces * cut.rows(kThreads) / kF8Block * kF8Block;   // rows of a launch
     if (step < 1) return hipErrorInvalidConfiguration;
     for (int64_t at = 0; at < m.rows; at += step) {
         F8Mat part = from_row(m, at);

@@ -292,3 +292,71 @@ def test_on_another_stream_and_twice(lib, torch):
     torch.cuda.synchronize()
     for got, got2 in outs:
         assert torch.equal(got, want) and torch.equal(got2, want2)
+
+
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+@pytest.mark.parametrize("q,s", [(40, 70), (300, 3)])
+def test_sums_longer_than_one_chain(lib, torch, q, s, y):
+    """600000 terms, 4688 blocks; whole numbers of at most 4 whose sums stay below 2^24."""
+    rng = np.random.default_rng(q)
+    r = 600000
+    pick = np.array([c for c, v in enumerate(format_values(8)) if np.isfinite(v) and v == round(v) and abs(v) <= 4], dtype=np.uint8)
+
+    def side(rows):
+        codes = pick[rng.integers(0, len(pick), (rows, -(-r // 128) * 128))]
+        codes[:, r:] = 0
+        v = torch.from_numpy(format_values(8)[codes].astype(np.float32)).cuda()[:, :r]
+        return lib.F8Matrix(torch.from_numpy(codes).cuda(), torch.ones(-(-r // 128), rows, device="cuda"), rows, r, 1), v
+
+    A, av = side(q)
+    X, xv = side(s)
+    Y = torch.empty(s, q, dtype=torch.bfloat16 if y == "bf16" else torch.float32, device="cuda")
+    lib.coded_f8_mm(A, X, Y, y_rows=True)
+    want = (xv.double() @ av.double().t()).to(Y.dtype)
+    assert torch.equal(Y, want)
+
+
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+def test_tiles_of_no_terms(lib, torch, y):
+    dt = torch.bfloat16 if y == "bf16" else torch.float32
+    A, X = lib.alloc_f8(300, 0, 128), lib.alloc_f8(280, 0)
+    Y, C = torch.full((280, 300), 9.0, dtype=dt, device="cuda"), torch.randn(300, device="cuda").to(dt)
+    lib.coded_f8_mm(A, X, Y, y_rows=True, beta=1.0, C=C)
+    assert torch.equal(Y, C.expand(280, 300))
+
+
+def test_a_matrix_times_itself(lib, torch):
+    rng = np.random.default_rng(8)
+    for rows in (20, 300):
+        A, av = stored(lib, torch, rng, rows, 390, 1)
+        Y = torch.empty(rows, rows, device="cuda")
+        lib.coded_f8_mm(A, A, Y)
+        want, size, _ = limits(av, av)
+        # not symmetric to the bit: a sum t meets two scales one after the other, and fl(fl(t a) b) is not fl(fl(t b) a)
+        assert np.all(np.abs(host(Y) - want) <= 200 * 2.0 ** -23 * size)
+
+
+@pytest.mark.parametrize("q,r,s", [(65, 300, 33), (300, 640, 300)])
+def test_two_results_at_once_share_nothing(lib, torch, q, r, s):
+    """A workspace given by the caller; the same product twice into two results, and rows behind the last left as they were."""
+    rng = np.random.default_rng(9)
+    A, _ = stored(lib, torch, rng, q, r, 128)
+    X, _ = stored(lib, torch, rng, s, r, 1)
+    n = max(16, lib.coded_f8_workspace(q, r, s, lib.CODED_F32, False))
+    outs = [torch.full((q + 3, s), 5.0, device="cuda") for _ in range(2)]
+    for out in outs:
+        lib.coded_f8_mm(A, X, out[:q], workspace=torch.empty(n, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(outs[0], outs[1]) and bool((outs[0][q:] == 5).all())
+
+
+def test_many_short_rows_are_read_back(lib, torch):
+    """More rows than one launch's workgroups take where rows lie side by side in them, and rows cut into pieces."""
+    for q, r in ((1 << 20, 3), (3, 70000)):
+        a = torch.randn(q, r, device="cuda")
+        for block in (1, 128):
+            M = lib.alloc_f8(q, r, block)
+            lib.coded_f8_quantize(a, M)
+            out = torch.empty(q, r, device="cuda")
+            lib.coded_f8_dequantize(M, out)
+            s = M.scales.t().repeat_interleave(block, 0)[:q].repeat_interleave(128, 1)[:, :r]
+            assert bool(((out - a).abs() <= (2.0 ** -4 + 2.0 ** -20) * a.abs() + s * 2.0 ** -10).all())
