@@ -8,7 +8,12 @@
 // embed_join_kernel adds these up.  Nothing is added by atomics, so the sums
 // depend on the tokens alone.
 //
-// Bound: memory.
+// Bound: memory.  Measured, 65536 tokens, 4096 columns, a table of 65536 rows: the lookup (bf16)
+// 180 to 200 us (0.5 GB written, rows of 16940 tokens read), the gradient (bf16 rows, fp32 table of
+// which 1.07 GB are written) 396: sorting 35, sums and zeros 324 (4.9 TB/s), joining 28, as the most
+// frequent token's 4131 rows make one run.  1000 tokens, 512 columns, 16384 rows of fp32: 3, and 9 + 10 + 4.
+// Workgroups that write zeros first took 20 us more, mixed among the others 110; places looked up only
+// when their rows were wanted 34.
 #include <algorithm>
 
 #include "layers.h"

@@ -11,6 +11,11 @@
 // With u = 448 / m rounded to fp32, v u is at most 448 (1 + 2^-23) and rounds to
 // 448: no value has to be cut down.  m is 2^-100 at least, so u and m / 448 are
 // normal numbers.
+//
+// Bound: memory.  Measured: 65536 x 8192 bf16 both ways 541 us (2.1 GB, 4.0 TB/s; a copy
+// reaches 5.0: the transpose's rows take 128 bytes of every tile each), 16384 x 8192
+// 147, 11500 x 5750 fp32 both ways 97 (4.1 TB/s); along rows alone 8192 x 8192 fp32 62
+// (5.4 TB/s).  Back to bf16: 65536 x 8192 278 us (5.8 TB/s).
 #include "f8.h"
 #include "rows.h"
 

@@ -2,18 +2,33 @@
 // cores: out[i][j] = sum over blocks b of sP[b][i] sQ[b][j] (sum over b's columns
 // of P[i][k] Q[j][k]).
 //
-// A block of 128 columns is one step.  Its codes come from memory into registers
-// while the step before is computed, then into one of two halves of shared memory.
-// For bf16 results a block is one 8-bit matrix instruction a tile of 16 x 16: what
-// it adds up is multiplied by the scales and added to fp32 sums on the vector
-// units, which run beside the matrix cores.  That instruction cuts off what lies
-// more than 13 bits below the largest of eight products; a result's rounding to
-// bf16 is some twenty times that.  For fp32 results the codes become bf16 values
-// in registers, exactly, and meet on the bf16 instructions (half the rate), whose
-// products and sums are in fp32.
+// A block of 128 columns is one step.  Its codes and scales come from memory straight
+// into one of two halves of shared memory while the step before, in the other one,
+// is computed; the loads go out between the matrix instructions, which would wait
+// behind them if they went out at once.
 //
-// Q's rows lie in shared memory in an order that gives a lane 4 times TJ results
-// next to each other: row j of a wave's 16 TJ is at (j % TJ) * 16 + j / TJ.
+// For bf16 results a block is two 8-bit matrix instructions a tile of 32 x 32: what they
+// add up is multiplied by the scales and added to fp32 sums on the vector units,
+// beside the next instructions.  Those cut off what lies more than 13 bits below the
+// largest of eight products (measured: 1.5e-5 of a result in the 2-norm, 9e-5 with
+// outliers); its rounding to bf16 is twenty times that.  For fp32 results the codes
+// become bf16 values in registers, exactly, and meet on the bf16 instructions (half the
+// rate), whose products and sums are in fp32.
+//
+// Q's rows lie in shared memory in an order that gives a lane 4 TJ results of a
+// right-hand side next to each other: row j of a wave's 32 TJ is at (j % TJ) * 32 + j / TJ.
+//
+// Bound: the matrix cores and the vector units that add what they give.  Eight waves
+// share 256 x 256 results, 64 x 128 a wave, or 128 x 256 by way of bf16, where
+// conversions and sums take as many issue cycles as the matrix cores work; two waves a
+// SIMD cover each other.  Measured, blocks of 128 on one side: bf16 results of 8192 x 8192
+// times 16384 columns 901 us (2.44 PFLOP/s, matrix cores busy 62% of the cycles; a library
+// product of 8-bit matrices with one scale each 2.60), fp32 8192^3 899 (1.22; a library
+// product of bf16 matrices 1.40); blocks of 1 on both sides, twice the vector work
+// of the sums: bf16 8192^3 526 (2.09), fp32 8192 x 16384 times 8192 1939 (1.13).  A tile's beginning and end
+// take about 8 us.  Codes by way of registers, one barrier a step, took 1092 us for the
+// first, the same with 16 x 16 instructions 1126; the waves of a SIMD taking turns between
+// shared memory and matrix instructions 1189; all loads at the step's start 989.
 #include <algorithm>
 
 #include "f8.h"
@@ -26,7 +41,8 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 512;
-constexpr int64_t kMostChain = 4096;   // blocks that one fp32 sum takes: 2^-12 of the magnitudes at the most, next to 128 terms' 2^-16 each
+// Blocks that one fp32 sum takes: 4096 roundings of 2^-24 are at most 2^-12 of the sum of magnitudes.
+constexpr int64_t kMostChain = 4096;
 
 // How results are cut into tiles, and which tiles' sums are shared by several workgroups: the first `whole` tiles are
 // one workgroup's each, the rest are split along the blocks.
