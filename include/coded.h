@@ -587,7 +587,8 @@ coded_status coded_mx_mm_t(coded_dtype fmt, const void* codes, int64_t ldc, cons
  *           rows' number of blocks; 4-byte aligned).  NaN: a block without
  *           values, each of them counts as NaN.
  * Any run of rows that begins at a multiple of block_rows is such a matrix from
- * its first row and first scale on.  Sizes up to 2^40 each; any may be 0.
+ * its first row and first scale on.  Sizes up to 2^40 each, any may be 0;
+ * storing and reading back take up to 2^27 columns, products see below.
  */
 
 /* The smallest pitches of a q x r matrix: bytes between rows of codes, elements
@@ -653,7 +654,7 @@ coded_status coded_f8_mm(int64_t q, int64_t r, int64_t s, int32_t block_rows, co
  *            ldcc, ldo).  x times 1 / (1 - p), rounded to fp32, plus C is formed
  *            in fp32 and rounded once.  Dropped infinities and NaN are dropped.
  *   p        in [0, 1]; 1 drops everything.
- *   draw     below 2^56.  first_row in [0, 2^40], q and r up to 2^40.
+ *   draw     below 2^56.  first_row in [0, 2^40], q up to 2^40, r up to 2^33.
  * X or C may be out itself, with its stride; they must not overlap it otherwise.
  */
 coded_status coded_dropout(coded_dtype dt, const void* X, int64_t q, int64_t r, int64_t ldx, double p, uint64_t seed,
@@ -667,7 +668,7 @@ coded_status coded_dropout(coded_dtype dt, const void* X, int64_t q, int64_t r, 
  *   skip      a token whose rows are zero and get no gradient (padding); one
  *             that is no row of the table, -1 for example, skips none.
  * Table and rows are CODED_F32 or CODED_BF16, each its own; vocab up to 2^31 - 2
- * rows, n up to 2^31 - 1, d up to 2^40.
+ * rows, n up to 2^31 - 1, d up to 2^33.
  */
 
 /* out[i] = scale * E[tok[i]] (n x d; scale, the product in fp32, rounded once).

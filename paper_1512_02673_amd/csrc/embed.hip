@@ -11,7 +11,7 @@
 // Bound: memory.  Measured, 65536 tokens, 4096 columns, a table of 65536 rows: the lookup (bf16)
 // 180 to 200 us (0.5 GB written, rows of 16940 tokens read), the gradient (bf16 rows, fp32 table of
 // which 1.07 GB are written) 396: sorting 35, sums and zeros 324 (4.9 TB/s), joining 28, as the most
-// frequent token's 4131 rows make one run.  1000 tokens, 512 columns, 16384 rows of fp32: 3, and 9 + 10 + 4.
+// frequent token's 4131 rows make one run.  1000 tokens, 512 columns, 16384 rows of fp32: 3, and 5 + 10 + 4.
 // Workgroups that write zeros first took 20 us more, mixed among the others 110; places looked up only
 // when their rows were wanted 34.
 #include <algorithm>
@@ -53,22 +53,21 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a, RowCut cut
 // ---------------------------------------------------------------- sorting
 
 // Token i's place is the number of tokens with a lower row, and of earlier ones with the same.  A workgroup places
-// 64 tokens; each of its waves compares them with a quarter of all.
+// 64 tokens; each of its sixteen waves compares them with a sixteenth of all (four waves: 9.3 us for 1000 tokens).
+constexpr int kCountWaves = 16;
 template <bool WIDE>
-__global__ __launch_bounds__(kThreads) void embed_count_kernel(const void* tok, int n, int64_t vocab, int64_t skip, uint32_t* keys,
-                                                              uint32_t* index) {
+__global__ __launch_bounds__(kCountWaves * 64) void embed_count_kernel(const void* tok, int n, int64_t vocab, int64_t skip, uint32_t* keys,
+                                                                     uint32_t* index) {
     __shared__ __attribute__((aligned(16))) uint32_t all[kSmall];
-    __shared__ int before[4][64];
+    __shared__ int before[kCountWaves][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int padded = (n + 15) / 16 * 16;
-#pragma unroll 4
-    for (int i = tid; i < padded; i += kThreads) all[i] = i < n ? row_of<WIDE>(tok, i, vocab, skip) : 0xFFFFFFFFu;
+    const int each = (n + 4 * kCountWaves - 1) / (4 * kCountWaves) * 4;   // of all, a wave's: whole pieces of 16 bytes
+    for (int i = tid; i < each * kCountWaves; i += kCountWaves * 64) all[i] = i < n ? row_of<WIDE>(tok, i, vocab, skip) : 0xFFFFFFFFu;
     __syncthreads();
     const int i = blockIdx.x * 64 + lane;
     const uint32_t mine = i < n ? all[i] : 0u;
-    const int quarter = padded / 4;
     int count = 0;
-    for (int j = wave * quarter; j < (wave + 1) * quarter; j += 4) {
+    for (int j = wave * each; j < (wave + 1) * each; j += 4) {
         const u32x4_t k = *reinterpret_cast<const u32x4_t*>(all + j);
 #pragma unroll
         for (int e = 0; e < 4; ++e) count += k[e] < mine + (j + e < i ? 1u : 0u);
@@ -76,7 +75,9 @@ __global__ __launch_bounds__(kThreads) void embed_count_kernel(const void* tok, 
     before[wave][lane] = count;
     __syncthreads();
     if (wave == 0 && i < n) {
-        const int at = before[0][lane] + before[1][lane] + before[2][lane] + before[3][lane];
+        int at = 0;
+#pragma unroll
+        for (int w = 0; w < kCountWaves; ++w) at += before[w][lane];
         keys[at] = mine;
         index[at] = static_cast<uint32_t>(i);
     }
@@ -381,7 +382,7 @@ hipError_t sort_tokens(const EmbedGradArgs& a, const Plan& p, uint32_t*& keys, u
     keys = k[0];
     index = x[0];
     if (a.n <= kSmall) {
-        embed_count_kernel<WIDE><<<dim3(static_cast<uint32_t>(ceil_div(a.n, 64))), kThreads, 0, st>>>(a.tok, static_cast<int>(a.n), a.vocab, a.skip, keys, index);
+        embed_count_kernel<WIDE><<<dim3(static_cast<uint32_t>(ceil_div(a.n, 64))), kCountWaves * 64, 0, st>>>(a.tok, static_cast<int>(a.n), a.vocab, a.skip, keys, index);
         return hipGetLastError();
     }
     uint32_t* counts = reinterpret_cast<uint32_t*>(ws + 4 * p.list);

@@ -9,7 +9,8 @@
 namespace coded {
 namespace {
 
-constexpr int64_t kMostTerms = int64_t(1) << 23, kMostPitch = int64_t(1) << 24;
+constexpr int64_t kMostTerms = int64_t(1) << 23, kMostPitch = int64_t(1) << 24;   // of a product
+constexpr int64_t kMostStored = int64_t(1) << 27;                                  // columns of a matrix that is stored or read back
 
 int64_t code_pitch(int64_t r) { return ceil_div(r, kF8Block) * kF8Block; }
 
@@ -72,6 +73,7 @@ coded_status coded_f8_quantize(coded_dtype dt, const void* A, int64_t q, int64_t
         if (st == CODED_OK && cols) st = check_f8("MT", t_block_rows, t_codes, ldtc, t_scales, ldts, r, q, t);
         if (st != CODED_OK) return st;
         if (q == 0 || r == 0) return CODED_OK;
+        if (r > kMostStored) return fail(CODED_ERR_UNSUPPORTED, "r must be <= 2^27");
         if (!rows && !cols) return fail(CODED_ERR_ARG, "neither A's codes nor its transpose's are given");
         const hipError_t e = launch_f8_quantize(A, dt == CODED_BF16, q, r, lda, rows ? &m : nullptr, cols ? &t : nullptr,
                                                 static_cast<hipStream_t>(stream));
@@ -87,6 +89,7 @@ coded_status coded_f8_dequantize(int64_t q, int64_t r, int32_t block_rows, const
         if (st == CODED_OK) st = check_dense("out", dt, out, q, r, ldo);
         if (st != CODED_OK) return st;
         if (q == 0 || r == 0) return CODED_OK;
+        if (r > kMostStored) return fail(CODED_ERR_UNSUPPORTED, "r must be <= 2^27");
         const hipError_t e = launch_f8_dequantize(m, r, out, dt == CODED_BF16, ldo, static_cast<hipStream_t>(stream));
         return e == hipSuccess ? CODED_OK : hip_fail(e, "coded_f8_dequantize");
     });

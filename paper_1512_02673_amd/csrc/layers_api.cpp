@@ -12,8 +12,12 @@ namespace {
 constexpr uint64_t kDropoutStream = 10;   // of the seed's generator
 constexpr double kTop = std::numeric_limits<float>::max();
 
-coded_status check_sizes(int64_t a, int64_t b) {
-    return a < 0 || b < 0 || std::max(a, b) > kMostSize ? fail(CODED_ERR_SHAPE, "sizes must be in [0, 2^40]") : CODED_OK;
+constexpr int64_t kMostColumns = int64_t(1) << 33;
+
+coded_status check_sizes(int64_t rows, int64_t columns) {
+    if (rows < 0 || columns < 0 || std::max(rows, columns) > kMostSize) return fail(CODED_ERR_SHAPE, "sizes must be in [0, 2^40]");
+    if (columns > kMostColumns) return fail(CODED_ERR_UNSUPPORTED, "rows must have <= 2^33 columns");
+    return CODED_OK;
 }
 
 coded_status check_tokens(const void* tok, int32_t token_bytes, int64_t n, int64_t vocab) {
@@ -67,7 +71,7 @@ coded_status coded_embed(coded_dtype e_dt, const void* E, int64_t vocab, int64_t
                          int64_t ldo, void* stream) {
     return guarded([&] {
         coded_status st = check_tokens(tok, token_bytes, n, vocab);
-        if (st == CODED_OK) st = check_sizes(d, 0);
+        if (st == CODED_OK) st = check_sizes(0, d);
         if (st == CODED_OK) st = check_dense("E", e_dt, E, vocab, d, lde);
         if (st == CODED_OK) st = check_dense("out", out_dt, out, n, d, ldo);
         if (st != CODED_OK) return st;
@@ -84,7 +88,7 @@ coded_status coded_embed_workspace(int64_t n, int64_t vocab, int64_t d, int64_t*
     return guarded([&] {
         if (!bytes) return fail(CODED_ERR_ARG, "bytes is NULL");
         coded_status st = check_tokens(bytes, 4, n, vocab);
-        if (st == CODED_OK) st = check_sizes(d, 0);
+        if (st == CODED_OK) st = check_sizes(0, d);
         if (st != CODED_OK) return st;
         *bytes = embed_workspace_bytes(n, vocab, d);
         return CODED_OK;
@@ -97,7 +101,7 @@ coded_status coded_embed_grad(coded_dtype g_dt, const void* G, int64_t n, int64_
                               void* stream) {
     return guarded([&] {
         coded_status st = check_tokens(tok, token_bytes, n, vocab);
-        if (st == CODED_OK) st = check_sizes(d, 0);
+        if (st == CODED_OK) st = check_sizes(0, d);
         if (st == CODED_OK) st = check_dense("G", g_dt, G, n, d, ldg);
         if (st == CODED_OK) st = check_dense("dE", e_dt, dE, vocab, d, ldde);
         if (st != CODED_OK) return st;

@@ -166,6 +166,18 @@ def test_gradient_refused(lib, change, status):
     assert lib.lib().coded_embed_grad(*{**GRAD, **change}.values()) == getattr(lib, "CODED_ERR_" + status)
 
 
+def test_wider_than_the_launches_reach(lib):
+    w = 2 ** 27 + 1
+    wide = {**STORE, "r": w, "lda": w, "ldc": 2 ** 27 + 128, "ldts": w}
+    assert lib.lib().coded_f8_quantize(*wide.values()) == lib.CODED_ERR_UNSUPPORTED
+    back = dict(q=3, r=w, br=1, codes=0x2000, ldc=2 ** 27 + 128, scales=0x3000, lds=3, dt=0, out=0x1000, ldo=w, stream=None)
+    assert lib.lib().coded_f8_dequantize(*back.values()) == lib.CODED_ERR_UNSUPPORTED
+    d = 2 ** 33 + 1
+    assert lib.lib().coded_dropout(*{**DROP, "r": d, "ldx": d, "ldo": d}.values()) == lib.CODED_ERR_UNSUPPORTED
+    assert lib.lib().coded_embed(*{**EMB, "d": d, "lde": d, "ldo": d}.values()) == lib.CODED_ERR_UNSUPPORTED
+    assert lib.lib().coded_embed_grad(*{**GRAD, "d": d, "ldg": d, "ldde": d}.values()) == lib.CODED_ERR_UNSUPPORTED
+
+
 # ---------------------------------------------------------------- the binding
 
 @pytest.fixture(scope="module")
