@@ -668,7 +668,8 @@ coded_status coded_dropout(coded_dtype dt, const void* X, int64_t q, int64_t r, 
  *   skip      a token whose rows are zero and get no gradient (padding); one
  *             that is no row of the table, -1 for example, skips none.
  * Table and rows are CODED_F32 or CODED_BF16, each its own; vocab up to 2^31 - 2
- * rows, n up to 2^31 - 1, d up to 2^33.
+ * rows, n up to 2^31 - 1, d up to 2^33 (a gradient
+ * whose n * d is above 2^35 may be CODED_ERR_UNSUPPORTED, before any launch).
  */
 
 /* out[i] = scale * E[tok[i]] (n x d; scale, the product in fp32, rounded once).

@@ -413,23 +413,26 @@ hipError_t sort_tokens(const EmbedGradArgs& a, const Plan& p, uint32_t*& keys, u
     return hipSuccess;
 }
 
+// Workgroups of the sums, of the joins, and table rows that a workgroup fills.
+int64_t sum_blocks(const Plan& p) { return ceil_div(p.chunks.count, p.cut.rows(kThreads)) * p.cut.pieces; }
+int64_t join_pieces(int64_t d) { return ceil_div(d, 512); }
+int64_t join_blocks(const Plan& p, int64_t d) { return std::max<int64_t>(0, p.chunks.count - 1) * join_pieces(d); }
+int64_t fill_rows(int64_t vocab) { return std::min<int64_t>(kThreads, std::max<int64_t>(1, vocab / 2048)); }
+
 template <bool G16, bool E16>
 hipError_t sum_rows(const EmbedGradArgs& a, Plan p, const uint32_t* keys, const uint32_t* index, hipStream_t st) {
     float* parts = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + 4 * p.list + kMostBlocks * kMostBins * 4);
     RunChunks& g = p.chunks;
     if (a.beta != 1.0f) {
-        g.fill_rows = std::min<int64_t>(kThreads, std::max<int64_t>(1, a.vocab / 2048));
+        g.fill_rows = fill_rows(a.vocab);
         g.fills = ceil_div(a.vocab, g.fill_rows);
     }
-    const int64_t blocks = g.fills + ceil_div(g.count, p.cut.rows(kThreads)) * p.cut.pieces;
+    const int64_t blocks = g.fills + sum_blocks(p);
     if (blocks == 0) return hipSuccess;
-    if (!grid_fits(blocks, kThreads)) return hipErrorInvalidConfiguration;
     embed_sum_kernel<G16, E16><<<dim3(static_cast<uint32_t>(blocks)), kThreads, 0, st>>>(a, keys, index, g, p.cut, parts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.count < 2) return e;
-    const int64_t pieces = ceil_div(a.d, 512), joins = (g.count - 1) * pieces;
-    if (!grid_fits(joins, kThreads)) return hipErrorInvalidConfiguration;
-    embed_join_kernel<E16><<<dim3(static_cast<uint32_t>(joins)), kThreads, 0, st>>>(a, keys, g, pieces, parts);
+    embed_join_kernel<E16><<<dim3(static_cast<uint32_t>(join_blocks(p, a.d))), kThreads, 0, st>>>(a, keys, g, join_pieces(a.d), parts);
     return hipGetLastError();
 }
 
@@ -457,6 +460,11 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t st) {
 }
 
 int64_t embed_workspace_bytes(int64_t n, int64_t vocab, int64_t d) { return n == 0 || d == 0 ? 0 : plan_of(n, vocab, d).bytes(); }
+
+bool embed_grad_fits(int64_t n, int64_t vocab, int64_t d) {
+    const Plan p = plan_of(n, vocab, d);
+    return grid_fits(ceil_div(vocab, fill_rows(vocab)) + sum_blocks(p), kThreads) && grid_fits(join_blocks(p, d), kThreads);
+}
 
 hipError_t launch_embed_grad(const EmbedGradArgs& a, hipStream_t st) {
     const Plan p = plan_of(a.n, a.vocab, a.d);

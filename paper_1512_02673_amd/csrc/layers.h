@@ -36,6 +36,8 @@ struct EmbedGradArgs {
     void* workspace;
 };
 int64_t embed_workspace_bytes(int64_t n, int64_t vocab, int64_t d);
+// Whether the launches take the sizes: asked before the first of them, which writes.
+bool embed_grad_fits(int64_t n, int64_t vocab, int64_t d);
 hipError_t launch_embed_grad(const EmbedGradArgs& a, hipStream_t st);
 
 }  // namespace coded

@@ -107,6 +107,7 @@ coded_status coded_embed_grad(coded_dtype g_dt, const void* G, int64_t n, int64_
         if (st != CODED_OK) return st;
         if (!(std::fabs(scale) <= kTop && std::fabs(beta) <= kTop)) return fail(CODED_ERR_ARG, "scale and beta must be finite in fp32");
         if (vocab == 0 || d == 0) return CODED_OK;
+        if (!embed_grad_fits(n, vocab, d)) return fail(CODED_ERR_UNSUPPORTED, "n * d is more than the launches reach (2^35 always fits)");
         const int64_t need = embed_workspace_bytes(n, vocab, d);
         if (need > 0) {
             if (!workspace || workspace_bytes < need)

@@ -178,6 +178,14 @@ def test_wider_than_the_launches_reach(lib):
     assert lib.lib().coded_embed_grad(*{**GRAD, "d": d, "ldg": d, "ldde": d}.values()) == lib.CODED_ERR_UNSUPPORTED
 
 
+@pytest.mark.parametrize("beta", [0.0, 1.0])
+def test_gradients_of_more_parts_than_a_launch_joins(lib, beta):
+    # 8192 tokens are 1024 chunks: 1023 joins of 2^24 / 512 pieces are more than a grid has, the sums before them are not
+    d = 2 ** 24
+    wide = {**GRAD, "n": 8192, "d": d, "ldg": d, "ldde": d, "beta": beta, "ws": 0x100000, "wsb": 2 ** 60}
+    assert lib.lib().coded_embed_grad(*wide.values()) == lib.CODED_ERR_UNSUPPORTED
+
+
 # ---------------------------------------------------------------- the binding
 
 @pytest.fixture(scope="module")
