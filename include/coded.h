@@ -673,7 +673,7 @@ coded_status coded_dropout(coded_dtype dt, const void* X, int64_t q, int64_t r, 
  */
 
 /* out[i] = scale * E[tok[i]] (n x d; scale, the product in fp32, rounded once).
- * The row of a token that is neither skip nor in [0, vocab) is NaN. */
+ * The row of a token outside [0, vocab) is NaN, also where skip is that number. */
 coded_status coded_embed(coded_dtype e_dt, const void* E, int64_t vocab, int64_t d, int64_t lde, const void* tok,
                          int32_t token_bytes, int64_t n, int64_t skip, double scale, coded_dtype out_dt, void* out,
                          int64_t ldo, void* stream);

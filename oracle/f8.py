@@ -77,10 +77,8 @@ def kept(q: int, r: int, p: float, seed: int, draw: int, first_row: int) -> np.n
 def embed(E: np.ndarray, tok: np.ndarray, scale: float, skip: int) -> np.ndarray:
     out = np.full((len(tok), E.shape[1]), math.nan)
     for i, t in enumerate(tok):
-        if t == skip:
-            out[i] = 0.0
-        elif 0 <= t < len(E):
-            out[i] = scale * E[t]
+        if 0 <= t < len(E):
+            out[i] = 0.0 if t == skip else scale * E[t]
     return out
 
 

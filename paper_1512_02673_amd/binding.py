@@ -916,7 +916,8 @@ def _tokens(tok):
 
 
 def coded_embed(E, tok, out, scale: float = 1.0, skip: int = -1, stream=None) -> None:
-    """out[i] = scale * E[tok[i]] (E: vocab x d, out: n x d); zero for the token `skip`, NaN for one that E lacks."""
+    """out[i] = scale * E[tok[i]] (E: vocab x d, out: n x d); zero for the token `skip`, NaN for one that E lacks
+    (-1 too: a skip that is no row of E skips none)."""
     vocab, d, lde, e_dt = _mx_dense(E, "E")
     n_out, d_out, ldo, out_dt = _mx_dense(out, "out")
     tp, size, n = _tokens(tok)

@@ -52,6 +52,13 @@ def test_oracle_mask_depends_on_place_alone():
     assert not np.array_equal(whole, of.kept(20, 7, 0.4, 5, 4, 100))
 
 
+def test_oracle_skip_that_is_no_row_skips_none():
+    E = np.array([[1.0], [2.0]])
+    assert list(of.embed(E, np.array([0, 1]), 3.0, 0)[:, 0]) == [0, 6]
+    for skip in (-1, 2):
+        assert np.array_equal(np.isnan(of.embed(E, np.array([0, -1, 2]), 3.0, skip)[:, 0]), [False, True, True])
+
+
 @pytest.mark.parametrize("q,r,block,want", [(0, 0, 1, (0, 0)), (1, 1, 1, (128, 1)), (300, 128, 128, (128, 3)), (129, 5750, 128, (5760, 2)), (7, 129, 1, (256, 7))])
 def test_sizes(lib, q, r, block, want):
     assert lib.coded_f8_sizes(q, r, block) == want

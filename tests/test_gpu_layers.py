@@ -138,6 +138,23 @@ def test_lookup(lib, torch, n, vocab, d, wide, pad, e_dt, o_dt):
     assert bool((wide_out[0] == 7).all()) and bool((wide_out[-1] == 7).all()) and bool((wide_out[:, d:] == 7).all())
 
 
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("skip", [-1, 9, -100])
+def test_a_skip_that_is_no_row_skips_none(lib, torch, skip, wide):
+    """Tokens that the table lacks give NaN, also where skip is the same number; -1 is what a call without a skip has."""
+    E = torch.arange(1.0, 9 * 20 + 1, device="cuda").view(9, 20)
+    tok = torch.tensor([3, -1, 0, 9, 8, -100], dtype=torch.int64 if wide else torch.int32, device="cuda")
+    for given in ({"skip": skip},) + (({},) if skip == -1 else ()):
+        out = torch.zeros(6, 20, device="cuda")
+        lib.coded_embed(E, tok, out, **given)
+        assert torch.equal(out[[0, 2, 4]], E[[3, 0, 8]]) and bool(out[[1, 3, 5]].isnan().all())
+        dE = torch.full_like(E, float("nan"))
+        lib.coded_embed_grad(torch.ones(6, 20, device="cuda"), tok, dE, **given)
+        want = torch.zeros_like(E)
+        want[[3, 0, 8]] = 1.0
+        assert torch.equal(dE, want)
+
+
 def tokens_of(rng, kind, n, vocab):
     if kind == "same":
         return np.full(n, vocab // 2)
