@@ -13,6 +13,8 @@ namespace coded {
 constexpr int kF8Block = 128;
 constexpr float kF8Top = 448.0f;
 constexpr uint32_t kF8Least = 27u << 23;   // 2^-100: the smallest magnitude that a scale is made from
+// Blocks that one workgroup adds up: 4096 roundings of 2^-24 are at most 2^-12 of the sum of magnitudes.
+constexpr int64_t kF8Chain = 4096;
 
 struct F8Mat {
     uint8_t* codes;

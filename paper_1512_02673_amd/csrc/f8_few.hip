@@ -8,7 +8,8 @@
 // rows of a block; no wave waits for another.  Codes become bf16 values in
 // registers, which is exact, and meet on the bf16 matrix instructions, whose
 // products and sums are in fp32, for results of either type.  Where there are few
-// workgroups the blocks are split among several, whose sums are joined in order.
+// workgroups, or more blocks than one chain of additions takes (kF8Chain: 1024 a
+// wave), the blocks are split among several, whose sums are joined in order.
 //
 // Measured, us: 65536 x 8192 times 1 and 16: 93 and 100 (5.8 and 5.4 TB/s; loads in
 // the operands' order, half rows, into registers 118 and 126, without non-temporal
@@ -181,7 +182,8 @@ Plan plan_of(const F8Args& a) {
     Plan p{};
     p.rt = ceil_div(a.o.q, 32) >= 512 ? 2 : 1;
     p.groups = ceil_div(a.o.q, 16 * p.rt);
-    const int64_t splits = std::max<int64_t>(1, std::min(ceil_div(a.blocks, 8), 512 / std::max<int64_t>(1, p.groups)));
+    const int64_t few = std::min(ceil_div(a.blocks, 8), 512 / std::max<int64_t>(1, p.groups));
+    const int64_t splits = std::max<int64_t>(1, std::max(few, ceil_div(a.blocks, kF8Chain)));
     p.per = std::max<int64_t>(1, ceil_div(a.blocks, splits));
     p.splits = std::max<int64_t>(1, ceil_div(a.blocks, p.per));
     return p;

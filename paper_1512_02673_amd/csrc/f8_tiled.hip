@@ -41,8 +41,6 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 512;
-// Blocks that one fp32 sum takes: 4096 roundings of 2^-24 are at most 2^-12 of the sum of magnitudes.
-constexpr int64_t kMostChain = 4096;
 
 // How results are cut into tiles, and which tiles' sums are shared by several workgroups: the first `whole` tiles are
 // one workgroup's each, the rest are split along the blocks.
@@ -441,9 +439,9 @@ Cut cut_of(const F8Args& a) {
             }
         }
     }
-    if (a.blocks > kMostChain) {   // every tile's sums in parts of at most kMostChain blocks
+    if (a.blocks > kF8Chain) {   // every tile's sums in parts of at most kF8Chain blocks
         best.whole = 0;
-        best.per = std::min(best.splits > 1 ? best.per : a.blocks, kMostChain);
+        best.per = std::min(best.splits > 1 ? best.per : a.blocks, kF8Chain);
         best.splits = ceil_div(a.blocks, best.per);
     }
     return best;

@@ -107,6 +107,15 @@ def test_product_needs_its_workspace(lib):
     assert lib.lib().coded_f8_mm(*{**a, "ws": 0x7008, "wsb": need}.values()) == lib.CODED_ERR_ARG
 
 
+@pytest.mark.parametrize("q,r,s", [(4100, 1 << 22, 1), (20000, 1 << 23, 16), (7, 1 << 22, 20000), (100000, (1 << 19) + 1, 1), (2000, 1 << 23, 1)])
+def test_few_right_hand_sides_have_bounded_chains(lib, q, r, s):
+    """One workgroup adds at most 4096 blocks: longer sums leave their parts in the workspace, however many results there are."""
+    for y in (lib.CODED_F32, lib.CODED_BF16):
+        for y_rows in (False, True):
+            parts = -(-r // 128 // 4096)
+            assert lib.coded_f8_workspace(q, r, s, y, y_rows) >= parts * q * s * 4
+
+
 def test_workspace_refused(lib):
     b = ctypes.c_int64()
     h = lib.lib()

@@ -316,6 +316,19 @@ def test_sums_longer_than_one_chain(lib, torch, q, s, y):
     assert torch.equal(Y, want)
 
 
+def test_many_results_of_sums_longer_than_one_chain(lib, torch):
+    """Ones times ones over 2^22 terms, scales 1 and 1 + 2^-12: a block's sum is 128 + 2^-5.  At most 4096 blocks to a
+    workgroup, 1024 to a wave, then four waves and eight workgroups: within (1024 + 4 + 8 + 2) 2^-24 of the sum.  With all
+    32768 blocks in one workgroup each wave's upper 4096 additions would lose half a step: 2^-13."""
+    q, r = 4100, 1 << 22
+    A = lib.F8Matrix(torch.full((q, r), 0x38, dtype=torch.uint8, device="cuda"), torch.ones(r // 128, -(-q // 128), device="cuda"), q, r, 128)
+    X = lib.F8Matrix(torch.full((1, r), 0x38, dtype=torch.uint8, device="cuda"), torch.full((r // 128, 1), 1 + 2.0 ** -12, device="cuda"), 1, r, 1)
+    Y = torch.zeros(q, device="cuda")
+    lib.coded_f8_mm(A, X, Y)
+    want = r * (1 + 2.0 ** -12)
+    assert np.all(np.abs(host(Y) - want) <= (1024 + 4 + 8 + 2) * 2.0 ** -24 * want)
+
+
 @pytest.mark.parametrize("y", ["f32", "bf16"])
 def test_tiles_of_no_terms(lib, torch, y):
     dt = torch.bfloat16 if y == "bf16" else torch.float32
