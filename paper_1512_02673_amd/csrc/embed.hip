@@ -323,7 +323,9 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedGradArgs a, co
 }
 
 // The sums of the runs that begin in a chunk and go on in the next.  A workgroup takes 512 columns of one chunk's; its
-// four waves take parts in turn.
+// four waves take parts in turn, and add up kMostParts of them, then such sums: at 2^31 tokens a chunk has 2048 rows, and a
+// chain of additions is at most 2048, 513 or 512 long, not the 2^18 of a wave's parts one after another.
+constexpr int kMostParts = 512;
 template <bool E16>
 __global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedGradArgs a, const uint32_t* keys, RunChunks g, int64_t pieces, float* parts) {
     __shared__ float sums[4][64][9];
@@ -338,12 +340,34 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedGradArgs a, c
     float sum[8] = {};
     if (c < a.d) {
         if (wave == 0) row_load<false>(part_of(parts, chunk, 1, a.d), c, a.d, sum);
+        const float* from = part_of(parts, chunk + 1 + wave, 0, a.d);
+        int left = static_cast<int>((last - chunk - wave + 3) / 4);   // every fourth part
+        const auto add_some = [&] {
+            const int some = left < kMostParts ? left : kMostParts;
+            left -= some;
 #pragma unroll 8
-        for (int64_t k = chunk + 1 + wave; k <= last; k += 4) {
-            float v[8];
-            row_load<false>(part_of(parts, k, 0, a.d), c, a.d, v);
+            for (int k = 0; k < some; ++k) {
+                float v[8];
+                row_load<false>(from, c, a.d, v);
+                from += 8 * a.d;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += v[e];
+                for (int e = 0; e < 8; ++e) sum[e] += v[e];
+            }
+        };
+        add_some();
+        if (left > 0) {
+            float* const all = sums[wave][lane];    // in shared memory: the loop needs the registers
+#pragma unroll
+            for (int e = 0; e < 8; ++e) all[e] = sum[e];
+            while (left > 0) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+                add_some();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) all[e] += sum[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = all[e];
         }
     }
 #pragma unroll

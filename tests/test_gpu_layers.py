@@ -235,6 +235,20 @@ def test_gradient_of_a_large_vocabulary(lib, torch):
     assert bool((out[0] == 3008).all()) and bool((out[1] == 0).all()) and bool(out[2].isnan().all())
 
 
+def test_gradient_of_one_token_without_end(lib, torch):
+    """2^24 rows of 1 + 2^-9 for one token.  A chunk's 64 rows, 512 chunks' sums in a wave's chain, 128 sums of those, and
+    the four waves' bound the error by (64 + 513 + 128 + 4) 2^-24 of the sum; each chunk's sum after another, 65536 a
+    wave, loses half a step 2^15 times in each: 2^-10."""
+    n, d = 1 << 24, 3
+    tok = torch.full((n,), 2, dtype=torch.int32, device="cuda")
+    G = torch.full((n, d), 1 + 2.0 ** -9, device="cuda")
+    dE = torch.empty(4, d, device="cuda")
+    lib.coded_embed_grad(G, tok, dE)
+    want = n * (1 + 2.0 ** -9)
+    assert np.all(np.abs(host(dE)[2] - want) <= (64 + 513 + 128 + 4) * 2.0 ** -24 * want)
+    assert bool((dE[[0, 1, 3]] == 0).all())
+
+
 def test_gradient_is_the_same_every_time(lib, torch):
     rng = np.random.default_rng(0)
     tok = torch.from_numpy(tokens_of(rng, "text", 20000, 5000)).cuda()
