@@ -196,6 +196,13 @@ def _memory_of(stream):
     return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
 
 
+def _given(workspace):
+    """(data, bytes) of a caller's workspace.  The elements of an expanded one are more than its memory holds."""
+    if not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 _DTYPE_CODES: dict = {}   # filled on first use: torch is imported late
 
 
@@ -706,7 +713,7 @@ def _mx_product(transposed, M, X, Y, x_rows, y_rows, alpha, beta, C, workspace, 
                     workspace = torch.empty(wsb, dtype=torch.uint8, device=Y.device)
             wsp = workspace.data_ptr()
     elif workspace is not None:
-        wsp, wsb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        wsp, wsb = _given(workspace)
     order = bool(x_rows) | bool(y_rows) << 1
     if transposed:
         _check(lib().coded_mx_mm_t(*M._args(), q, r, x_dt, xp, ldx, s, order, alpha, beta, cp, ldcc, Y.data_ptr(), y_dt,
@@ -874,16 +881,16 @@ def coded_f8_mm(A: F8Matrix, X: F8Matrix, Y, y_rows: bool = False, alpha: float 
         else:
             raise ValueError("C must have Y's shape, or be one row of it")
         cp = C.data_ptr()
+    wsp, wsb = None, 0
+    if not (workspace is None or isinstance(workspace, str)):
+        wsp, wsb = _given(workspace)
     _on_gpu(("Y", "A", "A", "X", "X", "C", "workspace"), (Y, A.codes, A.scales, X.codes, X.scales, C if beta != 0 else None,
                                                         None if isinstance(workspace, str) else workspace))
-    wsp, wsb = None, 0
     if isinstance(workspace, str):
         wsb = coded_f8_workspace(q, r, s, y_dt, y_rows)
         if wsb:
             workspace = _workspace(wsb, Y.device, stream)
             wsp = workspace.data_ptr()
-    elif workspace is not None:
-        wsp, wsb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _check(lib().coded_f8_mm(q, r, s, *A._args(), *X._args(), bool(y_rows) << 1, alpha, beta, cp, ldcc, Y.data_ptr(), y_dt, ldy,
                              wsp, wsb, _stream(stream)))
 
@@ -943,14 +950,14 @@ def coded_embed_grad(G, tok, dE, scale: float = 1.0, beta: float = 0.0, skip: in
     tp, size, n = _tokens(tok)
     if G.dim() != 2 or dE.dim() != 2 or (n_g, d_g) != (n, d):
         raise ValueError(f"G must be {n} rows of {d}")
-    _on_gpu(("G", "tok", "dE", "workspace"), (G, tok, dE, None if isinstance(workspace, str) else workspace))
     wsp, wsb = None, 0
+    if not (workspace is None or isinstance(workspace, str)):
+        wsp, wsb = _given(workspace)
+    _on_gpu(("G", "tok", "dE", "workspace"), (G, tok, dE, None if isinstance(workspace, str) else workspace))
     if isinstance(workspace, str):
         wsb = coded_embed_workspace(n, vocab, d)
         if wsb:
             workspace = _workspace(wsb, dE.device, stream)
             wsp = workspace.data_ptr()
-    elif workspace is not None:
-        wsp, wsb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _check(lib().coded_embed_grad(g_dt, G.data_ptr(), n, d, ldg, tp, size, vocab, skip, scale, beta, e_dt, dE.data_ptr(), ldde, wsp,
                                   wsb, _stream(stream)))

@@ -249,3 +249,18 @@ def test_binding_refuses_wrong_shapes(lib, torch):
                  lambda: lib.coded_embed_grad(x[:4], tok, x)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_a_workspace_must_be_as_long_as_its_elements_say(lib, torch):
+    """An expanded tensor's elements are more than its memory; a kernel would write behind it."""
+    one = torch.zeros(1, dtype=torch.uint8)
+    A, X = lib.alloc_f8(300, 16384, 128, device="cpu"), lib.alloc_f8(260, 16384, device="cpu")
+    M = lib.alloc_mx(16, 1 << 16, lib.CODED_MX4, device="cpu")
+    tok, rows = torch.zeros(9, dtype=torch.int64), torch.zeros(9, 8)
+    for ws in (one.expand(1 << 30), torch.zeros(1 << 20, 2, dtype=torch.uint8).t()):
+        for call in (lambda: lib.coded_f8_mm(A, X, torch.zeros(300, 260), workspace=ws),
+                     lambda: lib.coded_embed_grad(rows, tok, torch.zeros(20, 8), workspace=ws),
+                     lambda: lib.coded_mx_mm(M, torch.zeros(1 << 16), torch.zeros(16), workspace=ws),
+                     lambda: lib.coded_mx_mm_t(M, torch.zeros(16), torch.zeros(1 << 16), workspace=ws)):
+            with pytest.raises(ValueError, match="contiguous"):
+                call()
