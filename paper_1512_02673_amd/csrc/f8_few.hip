@@ -28,6 +28,9 @@ namespace coded {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int64_t kFew = 32, kFewStreamed = 16;   // right-hand sides; where Q's codes do not stay in the memory-side cache
+
+bool streamed(const F8Args& a) { return streams(a.o.q * a.blocks * kF8Block); }
 
 struct FewArgs {
     F8Args a;
@@ -191,9 +194,10 @@ Plan plan_of(const F8Args& a) {
 
 template <int PE, int RT>
 hipError_t launch_one(const FewArgs& g, int64_t groups, hipStream_t st) {
-    const bool ntl = streams(g.a.o.q * g.a.blocks * kF8Block);
-    const auto kernel = g.a.Q.block_rows != 1 ? (ntl ? f8_few_kernel<PE, RT, true, true> : f8_few_kernel<PE, RT, true, false>)
-                                              : (ntl ? f8_few_kernel<PE, RT, false, true> : f8_few_kernel<PE, RT, false, false>);
+    const bool blocked = g.a.Q.block_rows != 1;
+    auto kernel = blocked ? f8_few_kernel<PE, RT, true, false> : f8_few_kernel<PE, RT, false, false>;
+    if constexpr (8 * PE <= kFewStreamed)   // more right-hand sides of a streamed matrix are the tiles'
+        if (streamed(g.a)) kernel = blocked ? f8_few_kernel<PE, RT, true, true> : f8_few_kernel<PE, RT, false, true>;
     kernel<<<dim3(static_cast<uint32_t>(groups)), kThreads, 0, st>>>(g);
     return hipGetLastError();
 }
@@ -205,7 +209,7 @@ hipError_t launch_rows(const FewArgs& g, int rt, int64_t groups, hipStream_t st)
 
 }  // namespace
 
-bool f8_few_serves(const F8Args& a) { return a.o.s <= (streams(a.o.q * a.blocks * kF8Block) ? 16 : 32); }
+bool f8_few_serves(const F8Args& a) { return a.o.s <= (streamed(a) ? kFewStreamed : kFew); }
 
 int64_t f8_few_workspace_bytes(const F8Args& a) {
     const Plan p = plan_of(a);
