@@ -614,25 +614,30 @@ coded_status coded_f8_quantize(coded_dtype dt, const void* A, int64_t q, int64_t
 coded_status coded_f8_dequantize(int64_t q, int64_t r, int32_t block_rows, const void* codes, int64_t ldc,
                                  const float* scales, int64_t lds, coded_dtype dt, void* out, int64_t ldo, void* stream);
 
-/* Bytes of device workspace that coded_f8_mm needs for these sizes (0: none, NULL will do). */
+/* Bytes of device workspace that coded_f8_mm needs for these sizes (0: none, NULL will do).  Above 524288 terms it
+ * holds every result's sum in fp32 for each 4096 blocks. */
 coded_status coded_f8_workspace(int64_t q, int64_t r, int64_t s, coded_dtype y_dt, int32_t order, int64_t* bytes);
 
 /*
  * coded_f8_mm -- Y = alpha * A X^T + beta * C, A (q x r) and X (s x r, a
  * right-hand side a row) in 8 bits.
  *   order     CODED_Y_ROWS: Y is s x q, a right-hand side a row; else 0: q x s.
- *   y_dt      CODED_F32: codes' products and their sums are exact products and
- *             fp32 sums.  CODED_BF16: with more than a few right-hand sides and
- *             rows, the matrix instruction for 8 bits adds the products of each
- *             eight consecutive columns to 13 bits below the largest of them
- *             (at most 7 * 2^-13 of it off, a few 1e-5 of a result in the
- *             2-norm, where its rounding to bf16 is 1.7e-3); sums of blocks are
- *             in fp32 in either case, and so is what the scales, alpha and
- *             beta C add.
+ *   y_dt      CODED_F32: exact products of codes, added up in fp32.  CODED_BF16:
+ *             the same with up to 32 right-hand sides, or up to 32 rows of A
+ *             (16 where the other side has more than 256 MiB of codes).  With
+ *             more of both, the matrix instruction for 8 bits adds the products
+ *             of each eight consecutive columns to 13 bits below the largest of
+ *             them (at most 7 * 2^-13 of it off, a few 1e-5 of a result in the
+ *             2-norm, where its rounding to bf16 is 1.7e-3; so a token's results
+ *             may differ in the last place from those of a call with few), and
+ *             CODED_F32 is the way to fp32 sums.  Sums of blocks are in fp32 in
+ *             either case, and so is what the scales, alpha and beta C add; no
+ *             more than 4096 blocks are added in one chain.
  *   alpha, beta, C, ldcc, Y, ldy, workspace   as coded_mx_mm's.
  * r up to 2^23 and code pitches up to 2^24 bytes, else CODED_ERR_UNSUPPORTED.  A NaN reaches the
  * results whose sums it is part of and no other; so does a product of two
- * blocks' scales that is infinite in fp32.
+ * blocks' scales that is infinite in fp32.  One below 2^-126 may be rounded to
+ * fp32's subnormal numbers.
  */
 coded_status coded_f8_mm(int64_t q, int64_t r, int64_t s, int32_t block_rows, const void* codes, int64_t ldc,
                          const float* scales, int64_t lds, int32_t x_block_rows, const void* x_codes, int64_t ldxc,

@@ -21,8 +21,8 @@
 // Bound: the matrix cores and the vector units that add what they give.  Eight waves
 // share 256 x 256 results, 64 x 128 a wave, or 128 x 256 by way of bf16, where
 // conversions and sums take as many issue cycles as the matrix cores work; two waves a
-// SIMD cover each other.  Measured, blocks of 128 on one side: bf16 results of 8192 x 8192
-// times 16384 columns 901 us (2.44 PFLOP/s, matrix cores busy 62% of the cycles; a library
+// SIMD cover each other.  Measured in loops on one set of data, blocks of 128 on one side: bf16 results
+// of 8192 x 8192 times 16384 columns 901 us (2.44 PFLOP/s, matrix cores busy 62% of the cycles; a library
 // product of 8-bit matrices with one scale each 2.60), fp32 8192^3 899 (1.22; a library
 // product of bf16 matrices 1.40); blocks of 1 on both sides, twice the vector work
 // of the sums: bf16 8192^3 526 (2.09), fp32 8192 x 16384 times 8192 1939 (1.13).  A tile's beginning and end
