@@ -38,15 +38,15 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a, RowCut cut
     const int64_t c = ((blockIdx.x % cut.pieces << cut.log_tpr) + (threadIdx.x & ((1 << cut.log_tpr) - 1))) * 8;
     if (i >= a.n || c >= a.d) return;
     const int64_t t = WIDE ? static_cast<const int64_t*>(a.tok)[i] : static_cast<int64_t>(static_cast<const int32_t*>(a.tok)[i]);
-    const bool there = t >= 0 && t < a.vocab;   // a token that the table lacks is NaN, also where skip is that number
     float v[8];
-    if (there && t != a.skip) {
+    if (t != a.skip && t >= 0 && t < a.vocab) {
         row_load<E16>(static_cast<const char*>(a.E) + t * a.lde * (E16 ? 2 : 4), c, a.d, v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= a.scale;
-    } else {
+    } else {   // a token that the table lacks is NaN, also where skip is that number
+        const float none = t >= 0 && t < a.vocab ? 0.0f : __builtin_nanf("");
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = there ? 0.0f : __builtin_nanf("");
+        for (int k = 0; k < 8; ++k) v[k] = none;
     }
     row_store<O16>(static_cast<char*>(a.out) + i * a.ldo * (O16 ? 2 : 4), c, a.d, v);
 }
